@@ -303,6 +303,57 @@ TC_API double tc_kv_cache_fraction(int32_t n_text, int32_t n_vis, int32_t n_kept
  */
 TC_API int tc_probe_rates(void* ws, size_t ws_bytes, void* stream, float* rates);
 
+/* ---- behind the compression: rotary positions and the cache of keys and values -------------------------------------------
+ *
+ * What the layers behind the compression do with the shortened sequence and with the tokens that follow it.  The conventions
+ * above hold, with two additions: rows that carry strides (tc_strides) may be views, and lengths per sequence are device
+ * arrays, which are clamped where they are out of range, not reported.
+ */
+typedef enum { TC_ROPE_HALF = 0, TC_ROPE_INTERLEAVED = 1 } tc_rope_layout;
+/* the angle per position of pair i, theta_i = base^(-2 i / r), for contexts longer than the model was trained on:
+   TC_ROPE_PLAIN   theta_i
+   TC_ROPE_LINEAR  theta_i / factor
+   TC_ROPE_BASE    the base times factor^(r / (r - 2)): the fastest pair stays, the slowest turns `factor` times slower (r > 2)
+   TC_ROPE_BANDS   theta_i (g + (1 - g) / factor), g = clamp((turns - low) / (high - low), 0, 1), turns = original_len theta_i / 2 pi:
+                   pairs that turn often within the original length stay, those that do not turn `low` times are slowed */
+typedef enum { TC_ROPE_PLAIN = 0, TC_ROPE_LINEAR = 1, TC_ROPE_BASE = 2, TC_ROPE_BANDS = 3 } tc_rope_scaling;
+
+typedef struct {
+  int32_t head_dim;     /* d_h in {64, 128}                                                     */
+  int32_t rot_dim;      /* r: the first r elements of a head are rotated, the others copied; even, 2 .. d_h; 0 => d_h */
+  int32_t layout;       /* tc_rope_layout: pair i is (i, i + r/2) or (2 i, 2 i + 1)             */
+  int32_t scaling;      /* tc_rope_scaling                                                      */
+  float base;           /* > 1 (10000 for LLaMA)                                                */
+  float factor;         /* >= 1; read unless TC_ROPE_PLAIN                                      */
+  int32_t original_len; /* >= 1; read for TC_ROPE_BANDS                                         */
+  float low, high;      /* 0 <= low < high; read for TC_ROPE_BANDS                              */
+  float magnitude;      /* cosines and sines are multiplied by it; > 0; 0 => 1                  */
+} tc_rope;
+
+/* Strides of a [batch, head, row, d_h] tensor, in elements; the elements of a row are contiguous.  Every stride is >= 0 and a
+   multiple of 16 bytes (so [B, T, H, d_h] and parts of a packed projection will do); inputs may repeat rows (stride 0). */
+typedef struct {
+  int64_t batch, head, row;
+} tc_strides;
+
+/*
+ * Tables for any positions: cos[i][k] = magnitude cos(pos_ids[i] theta_k), k < r/2, sin alike; the angle in float64, rounded
+ * once.  One call serves every layer.
+ *   pos_ids  [n] int32      cos, sin [n, r/2] float
+ */
+TC_API int tc_rope_tables(const tc_rope* r, const int32_t* pos_ids, int64_t n, float* cos, float* sin, void* stream);
+
+/*
+ * Rotary positions of queries or keys, (a, b) the pairs of `layout`:
+ *     y_a = x_a cos - x_b sin,   y_b = x_b cos + x_a sin      (transposed != 0: sin negated, the gradient with respect to x)
+ *   x, y      [batch, n_heads, n_rows, d_h] with strides xs, ys; y may be x with the same strides, else they must not overlap
+ *   cos, sin  [batch, n_rows, r/2] float
+ * Products and sums in float32, rounded once.  `dtype` is that of x and y.  batch 0 .. 65536, n_heads 1 .. 1024, n_rows 0 .. 2^20.
+ */
+TC_API int tc_rope_apply(const tc_rope* r, int32_t dtype, int32_t batch, int32_t n_heads, int32_t n_rows, const void* x,
+                         const tc_strides* xs, const float* cos, const float* sin, void* y, const tc_strides* ys,
+                         int32_t transposed, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,10 +18,12 @@ _DTYPES = {"f32": TC_F32, "bf16": TC_BF16, "f16": TC_F16}
 TC_NORM_NONE, TC_NORM_MINMAX = 0, 1
 TC_EIG_F64, TC_EIG_F32 = 0, 1
 TC_EIG_AUTO, TC_EIG_JACOBI, TC_EIG_TRIDIAGONAL = 0, 1, 2
+TC_ROPE_HALF, TC_ROPE_INTERLEAVED = 0, 1
+TC_ROPE_PLAIN, TC_ROPE_LINEAR, TC_ROPE_BASE, TC_ROPE_BANDS = 0, 1, 2, 3
 
 SYMBOLS = ("tc_workspace_bytes", "tc_status_string", "tc_attn_output", "tc_ipgs_score", "tc_select_topk",
            "tc_merge", "tc_merge_noalloc", "tc_similarity", "tc_compress", "tc_profile_compress", "tc_probe_rates", "tc_info_rank",
-           "tc_assemble_sequence", "tc_kv_cache_fraction")
+           "tc_assemble_sequence", "tc_kv_cache_fraction", "tc_rope_tables", "tc_rope_apply")
 PROF_KINDS = ("attn", "attn_reduce", "gram", "jacobi_init", "jacobi_solve", "jacobi_update", "jacobi_update_u", "jacobi_sweep_end",
               "sigma", "ics", "combine", "topk", "rownorm", "sim", "assign", "average", "tridiag", "bisect", "twisted",
               "backtransform", "tridiag_update")
@@ -64,6 +66,23 @@ def params_for(w, batch=None, **overrides):
     return make_params(**kw)
 
 
+class tc_rope(ctypes.Structure):
+    _fields_ = [
+        ("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32),
+        ("base", ctypes.c_float), ("factor", ctypes.c_float), ("original_len", ctypes.c_int32), ("low", ctypes.c_float),
+        ("high", ctypes.c_float), ("magnitude", ctypes.c_float),
+    ]
+
+
+class tc_strides(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("head", ctypes.c_int64), ("row", ctypes.c_int64)]
+
+
+def make_rope(head_dim, rot_dim=0, layout=TC_ROPE_HALF, scaling=TC_ROPE_PLAIN, base=10000.0, factor=1.0, original_len=0, low=0.0,
+              high=0.0, magnitude=0.0):
+    return tc_rope(head_dim, rot_dim, layout, scaling, base, factor, original_len, low, high, magnitude)
+
+
 _lib = None
 
 
@@ -93,6 +112,9 @@ def load_library():
     lib.tc_info_rank.argtypes = [pp, vp, vp, ctypes.c_int32, ctypes.c_float, vp, vp, vp, vp, sz, vp]
     lib.tc_assemble_sequence.argtypes = [pp, vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp]
     lib.tc_kv_cache_fraction.argtypes = [ctypes.c_int32] * 5
+    rp, sp, i32 = ctypes.POINTER(tc_rope), ctypes.POINTER(tc_strides), ctypes.c_int32
+    lib.tc_rope_tables.argtypes = [rp, vp, ctypes.c_int64, vp, vp, vp]
+    lib.tc_rope_apply.argtypes = [rp, i32, i32, i32, i32, vp, sp, vp, vp, vp, sp, i32, vp]
     for name in SYMBOLS[2:]:
         getattr(lib, name).restype = ctypes.c_int
     lib.tc_kv_cache_fraction.restype = ctypes.c_double
@@ -235,3 +257,90 @@ def tc_assemble_sequence(p, H, X_out, kept_idx, H_new, pos_ids, rope_base=10000.
 
 def tc_kv_cache_fraction(n_text, n_vis, n_kept, n_layers, n_layers_before):
     return float(load_library().tc_kv_cache_fraction(n_text, n_vis, n_kept, n_layers, n_layers_before))
+
+
+# ---- behind the compression: the tensors' shapes are checked, and work goes to the device that holds them
+
+def _shape(name, t, shape, dtype, device):
+    if t.dtype != dtype:
+        raise ValueError("%s: expected %s, got %s" % (name, dtype, t.dtype))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s: expected shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if not t.is_cuda or t.device != device:
+        raise ValueError("%s: tensors must be on one GPU" % name)
+
+
+def _whole(name, t, shape, dtype, device):
+    """Address of a contiguous tensor (None for None)."""
+    if t is None:
+        return None
+    _shape(name, t, shape, dtype, device)
+    if not t.is_contiguous():
+        raise ValueError("%s: must be contiguous" % name)
+    return t.data_ptr()
+
+
+def _rows(name, t, shape, dtype, device):
+    """Address and strides of a [batch, head, row, d_h] view with contiguous rows."""
+    _shape(name, t, shape, dtype, device)
+    if t.stride(3) != 1:
+        raise ValueError("%s: the elements of a row must be contiguous" % name)
+    return t.data_ptr(), ctypes.byref(tc_strides(t.stride(0), t.stride(1), t.stride(2)))
+
+
+class _on(object):
+    """The device of a call: its current stream, or the caller's."""
+
+    def __init__(self, device, stream):
+        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+        self.device, self.stream = device, stream
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return torch.cuda.current_stream(self.device).cuda_stream if self.stream is None else self.stream
+
+    def __exit__(self, *args):
+        if self.guard is not None:
+            self.guard.__exit__(*args)
+
+
+def _device(name, t):
+    if not t.is_cuda:
+        raise ValueError("%s: tensors must be on the GPU" % name)
+    return t.device
+
+
+def _rot(r):
+    return r.rot_dim if r.rot_dim > 0 else r.head_dim
+
+
+def _dtype_of(name, t):
+    for code, dtype in ((TC_BF16, torch.bfloat16), (TC_F16, torch.float16), (TC_F32, torch.float32)):
+        if t.dtype == dtype:
+            return code
+    raise ValueError("%s: %s is no storage type" % (name, t.dtype))
+
+
+def tc_rope_tables(r, pos_ids, cos, sin, stream=None):
+    """cos, sin: the shape of pos_ids and r/2 behind it."""
+    dev = _device("pos_ids", pos_ids)
+    shape = tuple(pos_ids.shape) + (_rot(r) // 2,)
+    pos = _whole("pos_ids", pos_ids, pos_ids.shape, torch.int32, dev)
+    c, s = _whole("cos", cos, shape, torch.float32, dev), _whole("sin", sin, shape, torch.float32, dev)
+    with _on(dev, stream) as st:
+        _check(load_library().tc_rope_tables(ctypes.byref(r), pos, pos_ids.numel(), c, s, st))
+
+
+def tc_rope_apply(r, x, cos, sin, y=None, transposed=False, stream=None):
+    """x, y: [batch, heads, rows, head_dim] views; without y the rows of x are turned in place."""
+    dev = _device("x", x)
+    y = x if y is None else y
+    if x.dim() != 4 or x.shape[3] != r.head_dim:
+        raise ValueError("x: expected [batch, heads, rows, %d], got %s" % (r.head_dim, tuple(x.shape)))
+    B, H, T, _ = x.shape
+    px, xs = _rows("x", x, x.shape, x.dtype, dev)
+    py, ys = _rows("y", y, x.shape, x.dtype, dev)
+    c, s = (_whole(n, t, (B, T, _rot(r) // 2), torch.float32, dev) for n, t in (("cos", cos), ("sin", sin)))
+    with _on(dev, stream) as st:
+        _check(load_library().tc_rope_apply(ctypes.byref(r), _dtype_of("x", x), B, H, T, px, xs, c, s, py, ys, int(transposed), st))

@@ -1,0 +1,53 @@
+// What the translation units behind the compression share: rows of 16 bytes in each storage type, and the checks of rotary parameters.
+#pragma once
+#include "tc_internal.h"
+
+namespace tc {
+
+// N elements of storage type T in 16 bytes (T = uint16_t: bf16, f16_t: half).
+template <typename T> struct Vec16 {
+  static constexpr int N = 8;
+  __device__ static inline void unpack(const uint4& w, float* f) {
+    unpack2<T>(w.x, f, f + 1);
+    unpack2<T>(w.y, f + 2, f + 3);
+    unpack2<T>(w.z, f + 4, f + 5);
+    unpack2<T>(w.w, f + 6, f + 7);
+  }
+  __device__ static inline uint4 pack(const float* f) {
+    return uint4{pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]), pack2<T>(f[4], f[5]), pack2<T>(f[6], f[7])};
+  }
+  __device__ static inline float one(T v) {
+    float lo, hi;
+    unpack2<T>((uint32_t)__builtin_bit_cast(uint16_t, v), &lo, &hi);
+    return lo;
+  }
+  __device__ static inline T round(float f) { return __builtin_bit_cast(T, (uint16_t)pack2<T>(f, 0.f)); }
+};
+template <> struct Vec16<float> {
+  static constexpr int N = 4;
+  __device__ static inline void unpack(const uint4& w, float* f) {
+    f[0] = __uint_as_float(w.x); f[1] = __uint_as_float(w.y); f[2] = __uint_as_float(w.z); f[3] = __uint_as_float(w.w);
+  }
+  __device__ static inline uint4 pack(const float* f) {
+    return uint4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+  }
+  __device__ static inline float one(float v) { return v; }
+  __device__ static inline float round(float f) { return f; }
+};
+
+inline int elem_size(int dtype) { return dtype == TC_F32 ? 4 : 2; }
+inline bool known_dtype(int dtype) { return dtype == TC_F32 || dtype == TC_BF16 || dtype == TC_F16; }
+
+int check_rope(const tc_rope* r);  // tc_status
+inline int rope_dim(const tc_rope* r) { return r->rot_dim > 0 ? r->rot_dim : r->head_dim; }
+
+// Strides along which there is more than one entry (`output`: entries that are written, which must differ).
+inline bool bad_strides(const tc_strides* s, int esize, int batch, int heads, int rows, bool output) {
+  const int64_t v[3] = {s->batch, s->head, s->row};
+  const int n[3] = {batch, heads, rows};
+  for (int i = 0; i < 3; i++)
+    if (n[i] > 1 && (v[i] < 0 || v[i] > (int64_t(1) << 44) || v[i] * esize % 16 != 0 || (output && v[i] == 0))) return true;
+  return false;
+}
+
+}  // namespace tc

@@ -1,0 +1,239 @@
+// Rotary positions: the tables of any positions, and their application to the rows of heads.  Pair (a, b) of a row is the complex number
+// a + i b, a position turns it by its angle; the transposed turn is the gradient.
+#include <cmath>
+
+#include "cache_internal.h"
+
+namespace tc {
+
+int check_rope(const tc_rope* r) {
+  if (!r) return TC_ERR_NULL;
+  if ((r->head_dim != 64 && r->head_dim != 128) || r->rot_dim < 0 || r->rot_dim > r->head_dim || r->rot_dim % 2 != 0) return TC_ERR_SHAPE;
+  if ((r->layout != TC_ROPE_HALF && r->layout != TC_ROPE_INTERLEAVED) || r->scaling < TC_ROPE_PLAIN || r->scaling > TC_ROPE_BANDS ||
+      !(r->base > 1.f) || !std::isfinite(r->base) || !(r->magnitude >= 0.f) || !std::isfinite(r->magnitude))
+    return TC_ERR_PARAM;
+  if (r->scaling != TC_ROPE_PLAIN && (!(r->factor >= 1.f) || !std::isfinite(r->factor))) return TC_ERR_PARAM;
+  if (r->scaling == TC_ROPE_BASE && rope_dim(r) <= 2) return TC_ERR_PARAM;
+  if (r->scaling == TC_ROPE_BANDS &&
+      (r->original_len < 1 || !(r->low >= 0.f) || !(r->high > r->low) || !std::isfinite(r->high)))
+    return TC_ERR_PARAM;
+  return TC_OK;
+}
+
+// One thread has one pair's angle per position and goes over some positions.
+__global__ __launch_bounds__(256) void rope_tables_kernel(const int32_t* __restrict__ pos, long long n, float* __restrict__ c,
+                                                          float* __restrict__ s, int half, double log_base, int scaling, double factor,
+                                                          double original_len, double low, double high, double magnitude, int per) {
+  const int k = threadIdx.x % half, rows = 256 / half;
+  if ((int)threadIdx.x >= rows * half) return;
+  double theta = exp(-(double)k / (double)half * log_base);
+  if (scaling == TC_ROPE_LINEAR) theta /= factor;
+  if (scaling == TC_ROPE_BANDS) {
+    const double turns = original_len * theta * 0.15915494309189533577;  // 1 / 2 pi
+    const double g = fmin(fmax((turns - low) / (high - low), 0.0), 1.0);
+    theta *= g + (1.0 - g) / factor;
+  }
+  const long long first = (long long)blockIdx.x * per * rows + threadIdx.x / half;
+  for (int j = 0; j < per; j++) {
+    const long long i = first + (long long)j * rows;
+    if (i >= n) return;
+    double sn, cs;
+    sincos((double)pos[i] * theta, &sn, &cs);
+    c[i * half + k] = (float)(cs * magnitude);
+    s[i * half + k] = (float)(sn * magnitude);
+  }
+}
+
+// The elements of a head are dealt to threads in items: VEC: the 16-byte vectors of a pair of halves (or one, whose pairs are
+// neighbours), behind them vectors that are copied; else single pairs, behind them single elements.
+__host__ __device__ inline int rope_items(int dh, int r, int n16, bool inter, bool vec) {
+  if (vec) return inter ? dh / n16 : dh / n16 - r / (2 * n16);
+  return r / 2 + dh - r;
+}
+template <typename T>
+inline bool rope_vec(int r, bool inter) { return r % ((inter ? 1 : 2) * Vec16<T>::N) == 0; }
+
+// What an item needs of the tables, and the turn of a head's item.  `sign`: -1 for the transposed turn.
+template <typename T, bool INTER, bool VEC>
+struct RopeItem {
+  static constexpr int N = Vec16<T>::N, NT = VEC ? (INTER ? N / 2 : N) : 1;
+  float c[NT], s[NT];
+  int item, r;
+  bool turned;
+  __device__ inline RopeItem(const float* cs, const float* sn, int item_, int r_, float sign) : item(item_), r(r_) {
+    turned = item < (VEC ? (INTER ? r / N : r / (2 * N)) : r / 2);
+    if (turned) {
+#pragma unroll
+      for (int k = 0; k < NT; k++) {
+        c[k] = cs[item * NT + k];
+        s[k] = sign * sn[item * NT + k];
+      }
+    }
+  }
+  struct Data { uint4 a, b; };
+  __device__ inline void load(const T* x, Data& v) const {
+    if constexpr (VEC) {
+      const uint4* p = reinterpret_cast<const uint4*>(x);
+      v.a = p[INTER || turned ? item : item + r / (2 * N)];
+      if (!INTER && turned) v.b = p[item + r / (2 * N)];
+    } else {
+      v.a.x = __float_as_uint(Vec16<T>::one(x[turned ? (INTER ? 2 * item : item) : item + r / 2]));
+      if (turned) v.b.x = __float_as_uint(Vec16<T>::one(x[INTER ? 2 * item + 1 : item + r / 2]));
+    }
+  }
+  __device__ inline void turn(Data& v) const {
+    if (!turned) return;
+    if constexpr (VEC && INTER) {
+      float f[N];
+      Vec16<T>::unpack(v.a, f);
+#pragma unroll
+      for (int k = 0; k < NT; k++) {
+        const float a = f[2 * k], b = f[2 * k + 1];
+        f[2 * k] = a * c[k] - b * s[k];
+        f[2 * k + 1] = b * c[k] + a * s[k];
+      }
+      v.a = Vec16<T>::pack(f);
+    } else if constexpr (VEC) {
+      float a[N], b[N];
+      Vec16<T>::unpack(v.a, a);
+      Vec16<T>::unpack(v.b, b);
+#pragma unroll
+      for (int k = 0; k < NT; k++) {
+        const float x = a[k], y = b[k];
+        a[k] = x * c[k] - y * s[k];
+        b[k] = y * c[k] + x * s[k];
+      }
+      v.a = Vec16<T>::pack(a);
+      v.b = Vec16<T>::pack(b);
+    } else {
+      const float a = __uint_as_float(v.a.x), b = __uint_as_float(v.b.x);
+      v.a.x = __float_as_uint(a * c[0] - b * s[0]);
+      v.b.x = __float_as_uint(b * c[0] + a * s[0]);
+    }
+  }
+  __device__ inline void store(T* y, const Data& v) const {
+    if constexpr (VEC) {
+      uint4* p = reinterpret_cast<uint4*>(y);
+      p[INTER || turned ? item : item + r / (2 * N)] = v.a;
+      if (!INTER && turned) p[item + r / (2 * N)] = v.b;
+    } else {
+      y[turned ? (INTER ? 2 * item : item) : item + r / 2] = Vec16<T>::round(__uint_as_float(v.a.x));
+      if (turned) y[INTER ? 2 * item + 1 : item + r / 2] = Vec16<T>::round(__uint_as_float(v.b.x));
+    }
+  }
+};
+
+// Token, head and item of a thread: items fastest, then `groups` heads side by side, then tokens.
+struct RopeThread {
+  long long token;
+  int head, item;
+};
+__device__ inline RopeThread rope_thread(int items, int groups) {
+  const unsigned per = (unsigned)(items * groups);
+  const unsigned long long at = (unsigned long long)blockIdx.x * 256;
+  const unsigned long long t0 = at / per;
+  const unsigned off = (unsigned)(at - t0 * per) + threadIdx.x, in = off % per;
+  return {(long long)(t0 + off / per), (int)(in / (unsigned)items), (int)(in % (unsigned)items)};
+}
+
+// A thread keeps its item's part of the tables for PER heads: heads of a token read them once.
+template <typename T, bool INTER, bool VEC, int PER>
+__global__ __launch_bounds__(256) void rope_apply_kernel(const T* x, tc_strides xs, const float* __restrict__ c, const float* __restrict__ s,
+                                                         T* y, tc_strides ys, long long tokens, int rows, int heads, int groups, int items,
+                                                         int r, float sign) {
+  const RopeThread me = rope_thread(items, groups);
+  if (me.token >= tokens) return;
+  const long long b = me.token / rows, t = me.token % rows;
+  typedef RopeItem<T, INTER, VEC> Item;
+  const Item it(c + me.token * (r / 2), s + me.token * (r / 2), me.item, r, sign);
+  const T* xr = x + b * xs.batch + t * xs.row;
+  T* yr = y + b * ys.batch + t * ys.row;
+  typename Item::Data v[PER];
+#pragma unroll
+  for (int k = 0; k < PER; k++) {
+    const int h = me.head + k * groups;
+    if (h < heads) it.load(xr + h * xs.head, v[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < PER; k++) {
+    const int h = me.head + k * groups;
+    if (h < heads) {
+      it.turn(v[k]);
+      it.store(yr + h * ys.head, v[k]);
+    }
+  }
+}
+
+// Heads of a thread: four where the threads still fill the chip (256 compute units of 1024 threads).
+inline int rope_per(long long tokens, int heads, int items) {
+  return tokens * ((heads + 3) / 4) * items >= 256 * 1024 ? 4 : 1;
+}
+
+template <typename T, bool INTER, bool VEC>
+static int rope_launch(const tc_rope* p, int batch, int heads, int rows, const void* x, const tc_strides* xs, const float* c, const float* s,
+                       void* y, const tc_strides* ys, int transposed, hipStream_t st) {
+  const int r = rope_dim(p), items = rope_items(p->head_dim, r, Vec16<T>::N, INTER, VEC);
+  const long long tokens = (long long)batch * rows;
+  const int per = rope_per(tokens, heads, items), groups = (heads + per - 1) / per;
+  const long long blocks = (tokens * groups * items + 255) / 256;
+  if (blocks > 0x7fffffffLL) return TC_ERR_SHAPE;
+  const float sign = transposed ? -1.f : 1.f;
+  if (per == 4)
+    rope_apply_kernel<T, INTER, VEC, 4><<<(unsigned)blocks, 256, 0, st>>>((const T*)x, *xs, c, s, (T*)y, *ys, tokens, rows, heads, groups, items, r, sign);
+  else
+    rope_apply_kernel<T, INTER, VEC, 1><<<(unsigned)blocks, 256, 0, st>>>((const T*)x, *xs, c, s, (T*)y, *ys, tokens, rows, heads, groups, items, r, sign);
+  return check_launch();
+}
+
+// F<T, INTER, VEC>(args) for the storage type, the layout and whether the rotated part falls into vectors.
+#define TC_ROPE_CALL(F, dtype, p, ...)                                                                             \
+  [&]() -> int {                                                                                                   \
+    const bool inter = (p)->layout == TC_ROPE_INTERLEAVED;                                                         \
+    auto by = [&](auto tag) -> int {                                                                               \
+      typedef decltype(tag) T;                                                                                     \
+      if (rope_vec<T>(rope_dim(p), inter)) return inter ? F<T, true, true>(__VA_ARGS__) : F<T, false, true>(__VA_ARGS__); \
+      return inter ? F<T, true, false>(__VA_ARGS__) : F<T, false, false>(__VA_ARGS__);                             \
+    };                                                                                                             \
+    return (dtype) == TC_F32 ? by(0.f) : (dtype) == TC_BF16 ? by(uint16_t(0)) : by(f16_t{0});                      \
+  }()
+
+}  // namespace tc
+
+using namespace tc;
+
+extern "C" int tc_rope_tables(const tc_rope* r, const int32_t* pos_ids, int64_t n, float* cos, float* sin, void* stream) {
+  const int rc = check_rope(r);
+  if (rc != TC_OK) return rc;
+  if (n < 0 || n > (int64_t(1) << 36)) return TC_ERR_SHAPE;
+  if (n == 0) return TC_OK;
+  if (!pos_ids || !cos || !sin) return TC_ERR_NULL;
+  if (misaligned(pos_ids) || misaligned(cos) || misaligned(sin)) return TC_ERR_ALIGN;
+  const int rd = rope_dim(r), half = rd / 2, rows = 256 / half;
+  double log_base = std::log((double)r->base);
+  if (r->scaling == TC_ROPE_BASE) log_base += std::log((double)r->factor) * rd / (rd - 2.0);
+  const int64_t blocks1 = (n + rows - 1) / rows;
+  const int per = blocks1 >= 8192 ? 8 : 1;  // positions of a thread: its angle is worth keeping once the chip is full
+  const int64_t blocks = (blocks1 + per - 1) / per;
+  if (blocks > 0x7fffffffLL) return TC_ERR_SHAPE;
+  rope_tables_kernel<<<(unsigned)blocks, 256, 0, (hipStream_t)stream>>>(pos_ids, n, cos, sin, half, log_base, r->scaling, (double)r->factor,
+                                                                        (double)r->original_len, (double)r->low, (double)r->high,
+                                                                        r->magnitude > 0.f ? (double)r->magnitude : 1.0, per);
+  return check_launch();
+}
+
+extern "C" int tc_rope_apply(const tc_rope* r, int32_t dtype, int32_t batch, int32_t n_heads, int32_t n_rows, const void* x,
+                             const tc_strides* xs, const float* cos, const float* sin, void* y, const tc_strides* ys,
+                             int32_t transposed, void* stream) {
+  const int rc = check_rope(r);
+  if (rc != TC_OK) return rc;
+  if (!known_dtype(dtype)) return TC_ERR_DTYPE;
+  if (batch < 0 || batch > (1 << 16) || n_heads < 1 || n_heads > 1024 || n_rows < 0 || n_rows > (1 << 20)) return TC_ERR_SHAPE;
+  if (batch == 0 || n_rows == 0) return TC_OK;
+  if (!x || !xs || !cos || !sin || !y || !ys) return TC_ERR_NULL;
+  const int es = elem_size(dtype);
+  if (bad_strides(xs, es, batch, n_heads, n_rows, false) || bad_strides(ys, es, batch, n_heads, n_rows, true)) return TC_ERR_SHAPE;
+  if (misaligned(x) || misaligned(cos) || misaligned(sin) || misaligned(y)) return TC_ERR_ALIGN;
+  if (x == y && ((batch > 1 && xs->batch != ys->batch) || (n_heads > 1 && xs->head != ys->head) || (n_rows > 1 && xs->row != ys->row)))
+    return TC_ERR_PARAM;
+  return TC_ROPE_CALL(rope_launch, dtype, r, r, batch, n_heads, n_rows, x, xs, cos, sin, y, ys, transposed, (hipStream_t)stream);
+}
