@@ -354,6 +354,64 @@ TC_API int tc_rope_apply(const tc_rope* r, int32_t dtype, int32_t batch, int32_t
                          const tc_strides* xs, const float* cos, const float* sin, void* y, const tc_strides* ys,
                          int32_t transposed, void* stream);
 
+/*
+ * The cache of one layer, and one call on it.  Keys and values of sequence b lie in slots, K_cache, V_cache [B, H_kv, capacity, d_h]:
+ * len[b] of them are in use, slots 0 .. len[b]-1, in any order; slot_pos [B, H_kv, capacity] int32 says which position a slot's token
+ * has, weight [B, H_kv, capacity] float how much attention it has gathered.  The tokens of a call are the last q_len[b] of them, in
+ * their order (so tc_cache_append, then tc_cache_attention, with the same len and q_len; tc_cache_evict behind them).
+ *   len    [B] int32 device: slots in use, the tokens of the call among them; clamped to 0 .. max_len
+ *   q_len  [B] int32 device: tokens of the call, the first ones of n_query rows; clamped to 0 .. n_query; NULL: n_query everywhere
+ */
+typedef struct {
+  int32_t batch;        /* B: sequences, 0 .. 65536 (0: nothing is launched, TC_OK)             */
+  int32_t n_heads;      /* H: query heads, 1 .. 1024                                            */
+  int32_t n_kv_heads;   /* H_kv: a divisor of H; query head h reads key/value head h / (H/H_kv) */
+  int32_t head_dim;     /* d_h in {64, 128}                                                     */
+  int32_t dtype;        /* tc_dtype of queries, keys, values and outputs                        */
+  int32_t n_query;      /* T: rows of queries per sequence, 1 .. 2^20                           */
+  int32_t capacity;     /* slots per sequence and head, 1 .. 2^24                               */
+  int32_t max_len;      /* no len[b] of this call is larger (what the launch is sized by); 0 => capacity */
+  int32_t n_prefixes;   /* prefixes that sequences share, sequence b has number b / (B / n_prefixes): a divisor of B; 0 if none */
+  int32_t prefix_len;   /* P: keys of each prefix, 0 .. 2^24; 0 if there is none                */
+  float softmax_scale;  /* 0 => 1/sqrt(head_dim)                                                */
+  int32_t budget;       /* eviction: slots that stay in use at most, 1 .. capacity; 0 elsewhere  */
+  int32_t n_sink;       /* eviction: positions below it stay ...                                */
+  int32_t n_recent;     /* ... and the latest n_recent positions; n_sink, n_recent >= 0, n_sink + n_recent <= budget */
+} tc_cache;
+
+/* Bytes of scratch that any entry point may need for `c` (0 if c is invalid), whatever max_len is.  budget is looked at only by
+   tc_cache_evict: 0 will do elsewhere. */
+TC_API size_t tc_cache_workspace_bytes(const tc_cache* c);
+
+/*
+ * New tokens: queries and keys are turned by their positions (as by tc_rope_apply), keys and values go to their slots.
+ *   Q [B, H, T, d_h], K, V [B, H_kv, T, d_h]  views with strides qs, ks, vs (parts of a packed projection, say)
+ *   cos, sin  [B, T, r/2] float, from tc_rope_tables; r, cos and sin all NULL: nothing is turned
+ *   pos_ids   [B, T] int32
+ *   Q_out     [B, H, T, d_h]  written, contiguous; rows behind q_len[b] are zero
+ *   K_cache, V_cache, slot_pos, weight: row t < q_len[b] goes to slot len[b] - q_len[b] + t of every head, with position pos_ids[b, t] and
+ *             weight 0; a row whose slot is not within 0 .. capacity-1 is left out; other slots stay as they are
+ * No two tensors overlap.
+ */
+TC_API int tc_cache_append(const tc_cache* c, const tc_rope* r, const void* Q, const tc_strides* qs, const void* K, const tc_strides* ks,
+                           const void* V, const tc_strides* vs, const float* cos, const float* sin, const int32_t* pos_ids,
+                           const int32_t* len, const int32_t* q_len, void* Q_out, void* K_cache, void* V_cache, int32_t* slot_pos,
+                           float* weight, void* stream);
+
+/*
+ * Eviction: of every sequence and key/value head the `budget` best slots stay in use.  A slot whose position is below n_sink or above
+ * newest - n_recent (newest: the largest position in use) comes before the others, these come by weight, largest first (NaN last), equal
+ * ones by slot, lowest first.  Slots 0 .. budget-1 that stay keep what they hold; the others that stay go, in ascending order, to the
+ * slots that are freed there, in ascending order.  Where no more than `budget` slots are in use all of them stay.
+ *   K_out, V_out [B, H_kv, out_capacity, d_h], pos_out, weight_out [B, H_kv, out_capacity]: written up to len_out[b], left as they are behind
+ *             it; out_capacity >= budget.  In place: the four are the cache's own and out_capacity = capacity (only the rows that change slot
+ *             are touched); else none of them overlaps another tensor
+ *   len_out   [B] int32  min(len[b], budget); not len itself
+ */
+TC_API int tc_cache_evict(const tc_cache* c, const int32_t* len, const void* K_cache, const void* V_cache, const int32_t* slot_pos,
+                          const float* weight, void* K_out, void* V_out, int32_t* pos_out, float* weight_out, int32_t out_capacity,
+                          int32_t* len_out, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

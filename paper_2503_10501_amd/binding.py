@@ -23,7 +23,8 @@ TC_ROPE_PLAIN, TC_ROPE_LINEAR, TC_ROPE_BASE, TC_ROPE_BANDS = 0, 1, 2, 3
 
 SYMBOLS = ("tc_workspace_bytes", "tc_status_string", "tc_attn_output", "tc_ipgs_score", "tc_select_topk",
            "tc_merge", "tc_merge_noalloc", "tc_similarity", "tc_compress", "tc_profile_compress", "tc_probe_rates", "tc_info_rank",
-           "tc_assemble_sequence", "tc_kv_cache_fraction", "tc_rope_tables", "tc_rope_apply")
+           "tc_assemble_sequence", "tc_kv_cache_fraction", "tc_rope_tables", "tc_rope_apply",
+           "tc_cache_workspace_bytes", "tc_cache_append", "tc_cache_evict")
 PROF_KINDS = ("attn", "attn_reduce", "gram", "jacobi_init", "jacobi_solve", "jacobi_update", "jacobi_update_u", "jacobi_sweep_end",
               "sigma", "ics", "combine", "topk", "rownorm", "sim", "assign", "average", "tridiag", "bisect", "twisted",
               "backtransform", "tridiag_update")
@@ -78,6 +79,21 @@ class tc_strides(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int64), ("head", ctypes.c_int64), ("row", ctypes.c_int64)]
 
 
+class tc_cache(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("n_query", ctypes.c_int32), ("capacity", ctypes.c_int32), ("max_len", ctypes.c_int32),
+        ("n_prefixes", ctypes.c_int32), ("prefix_len", ctypes.c_int32), ("softmax_scale", ctypes.c_float),
+        ("budget", ctypes.c_int32), ("n_sink", ctypes.c_int32), ("n_recent", ctypes.c_int32),
+    ]
+
+
+def make_cache(batch, n_heads, n_kv_heads, head_dim, dtype, n_query, capacity, max_len=0, n_prefixes=0, prefix_len=0,
+               softmax_scale=0.0, budget=0, n_sink=0, n_recent=0):
+    return tc_cache(batch, n_heads, n_kv_heads, head_dim, dtype, n_query, capacity, max_len, n_prefixes, prefix_len, softmax_scale,
+                    budget, n_sink, n_recent)
+
+
 def make_rope(head_dim, rot_dim=0, layout=TC_ROPE_HALF, scaling=TC_ROPE_PLAIN, base=10000.0, factor=1.0, original_len=0, low=0.0,
               high=0.0, magnitude=0.0):
     return tc_rope(head_dim, rot_dim, layout, scaling, base, factor, original_len, low, high, magnitude)
@@ -115,8 +131,13 @@ def load_library():
     rp, sp, i32 = ctypes.POINTER(tc_rope), ctypes.POINTER(tc_strides), ctypes.c_int32
     lib.tc_rope_tables.argtypes = [rp, vp, ctypes.c_int64, vp, vp, vp]
     lib.tc_rope_apply.argtypes = [rp, i32, i32, i32, i32, vp, sp, vp, vp, vp, sp, i32, vp]
+    cp = ctypes.POINTER(tc_cache)
+    lib.tc_cache_workspace_bytes.argtypes = [cp]
+    lib.tc_cache_append.argtypes = [cp, rp, vp, sp, vp, sp, vp, sp] + [vp] * 11
+    lib.tc_cache_evict.argtypes = [cp] + [vp] * 9 + [i32, vp, vp, sz, vp]
     for name in SYMBOLS[2:]:
         getattr(lib, name).restype = ctypes.c_int
+    lib.tc_cache_workspace_bytes.restype = sz
     lib.tc_kv_cache_fraction.restype = ctypes.c_double
     _lib = lib
     return lib
@@ -344,3 +365,59 @@ def tc_rope_apply(r, x, cos, sin, y=None, transposed=False, stream=None):
     c, s = (_whole(n, t, (B, T, _rot(r) // 2), torch.float32, dev) for n, t in (("cos", cos), ("sin", sin)))
     with _on(dev, stream) as st:
         _check(load_library().tc_rope_apply(ctypes.byref(r), _dtype_of("x", x), B, H, T, px, xs, c, s, py, ys, int(transposed), st))
+
+
+def tc_cache_workspace_bytes(c):
+    return int(load_library().tc_cache_workspace_bytes(ctypes.byref(c)))
+
+
+def new_cache_workspace(c, device="cuda"):
+    n = tc_cache_workspace_bytes(c)
+    if n == 0:
+        raise TokenCarveError(-4, "invalid tc_cache")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _cached(c, K_cache, V_cache, lens, q_len, dev):
+    """Addresses of what every call on a cache takes: keys, values, lengths."""
+    shape = (c.batch, c.n_kv_heads, c.capacity, c.head_dim)
+    sd = storage_dtype(c)
+    return (_whole("K_cache", K_cache, shape, sd, dev), _whole("V_cache", V_cache, shape, sd, dev),
+            _whole("lens", lens, (c.batch,), torch.int32, dev), _whole("q_len", q_len, (c.batch,), torch.int32, dev))
+
+
+def tc_cache_append(c, r, Q, K, V, cos, sin, pos_ids, lens, Q_out, K_cache, V_cache, slot_pos, weight, q_len=None, stream=None):
+    """Q [B, H, T, d], K, V [B, H_kv, T, d]: views; r, cos and sin None: nothing is turned."""
+    dev, sd = _device("Q", Q), storage_dtype(c)
+    B, T, d, slots = c.batch, c.n_query, c.head_dim, (c.batch, c.n_kv_heads, c.capacity)
+    q, qs = _rows("Q", Q, (B, c.n_heads, T, d), sd, dev)
+    k, ks = _rows("K", K, (B, c.n_kv_heads, T, d), sd, dev)
+    v, vs = _rows("V", V, (B, c.n_kv_heads, T, d), sd, dev)
+    co, si = (_whole(n, t, (B, T, _rot(r) // 2 if r is not None else 0), torch.float32, dev) for n, t in (("cos", cos), ("sin", sin)))
+    kc, vc, ln, ql = _cached(c, K_cache, V_cache, lens, q_len, dev)
+    pos, out = _whole("pos_ids", pos_ids, (B, T), torch.int32, dev), _whole("Q_out", Q_out, (B, c.n_heads, T, d), sd, dev)
+    sp, w = _whole("slot_pos", slot_pos, slots, torch.int32, dev), _whole("weight", weight, slots, torch.float32, dev)
+    with _on(dev, stream) as st:
+        _check(load_library().tc_cache_append(ctypes.byref(c), None if r is None else ctypes.byref(r), q, qs, k, ks, v, vs, co, si, pos, ln,
+                                              ql, out, kc, vc, sp, w, st))
+
+
+def tc_cache_evict(c, lens, K_cache, V_cache, slot_pos, weight, len_out, ws, K_out=None, V_out=None, pos_out=None, weight_out=None,
+                   stream=None):
+    """Without K_out, V_out, pos_out, weight_out [B, H_kv, out_capacity(, d)]: in place."""
+    dev, sd, slots = _device("K_cache", K_cache), storage_dtype(c), (c.batch, c.n_kv_heads, c.capacity)
+    kc, vc, ln, _ = _cached(c, K_cache, V_cache, lens, None, dev)
+    sp, w = _whole("slot_pos", slot_pos, slots, torch.int32, dev), _whole("weight", weight, slots, torch.float32, dev)
+    given = [t is not None for t in (K_out, V_out, pos_out, weight_out)]
+    if any(given) != all(given):
+        raise ValueError("K_out, V_out, pos_out and weight_out are given together")
+    cap = int(K_out.shape[2]) if all(given) and K_out.dim() == 4 else c.capacity
+    ko, vo, po, wo = kc, vc, sp, w
+    if all(given):
+        out = (c.batch, c.n_kv_heads, cap)
+        ko, vo = _whole("K_out", K_out, out + (c.head_dim,), sd, dev), _whole("V_out", V_out, out + (c.head_dim,), sd, dev)
+        po, wo = _whole("pos_out", pos_out, out, torch.int32, dev), _whole("weight_out", weight_out, out, torch.float32, dev)
+    lo = _whole("len_out", len_out, (c.batch,), torch.int32, dev)
+    work = _whole("ws", ws, ws.shape, torch.uint8, dev)
+    with _on(dev, stream) as st:
+        _check(load_library().tc_cache_evict(ctypes.byref(c), ln, kc, vc, sp, w, ko, vo, po, wo, cap, lo, work, ws.numel(), st))

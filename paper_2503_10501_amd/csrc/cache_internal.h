@@ -50,4 +50,23 @@ inline bool bad_strides(const tc_strides* s, int esize, int batch, int heads, in
   return false;
 }
 
+// A call on the cache, checked.
+struct CachePlan {
+  int B, H, Hk, G, dh, T, cap, max_len, images, each, P, esize;
+  int R;         // rows of queries per sequence and key/value head: the G heads that share it, T rows each, head after head
+  float scale;
+  int budget, sink, recent;
+  size_t total;  // bytes of workspace
+};
+int make_cache_plan(const tc_cache* c, CachePlan* plan);
+size_t evict_bytes(const CachePlan& pl);
+
+inline int check_cache_ws(const CachePlan& pl, const void* ws, size_t ws_bytes) {
+  if (!ws) return TC_ERR_NULL;
+  if (misaligned(ws)) return TC_ERR_ALIGN;
+  return ws_bytes < pl.total ? TC_ERR_WORKSPACE : TC_OK;
+}
+
+__device__ inline int clamp_len(int n, int most) { return n < 0 ? 0 : (n > most ? most : n); }
+
 }  // namespace tc

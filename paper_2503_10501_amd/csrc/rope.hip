@@ -62,7 +62,7 @@ struct RopeItem {
   bool turned;
   __device__ inline RopeItem(const float* cs, const float* sn, int item_, int r_, float sign) : item(item_), r(r_) {
     turned = item < (VEC ? (INTER ? r / N : r / (2 * N)) : r / 2);
-    if (turned) {
+    if (turned && cs) {
 #pragma unroll
       for (int k = 0; k < NT; k++) {
         c[k] = cs[item * NT + k];
@@ -178,20 +178,97 @@ static int rope_launch(const tc_rope* p, int batch, int heads, int rows, const v
   const long long blocks = (tokens * groups * items + 255) / 256;
   if (blocks > 0x7fffffffLL) return TC_ERR_SHAPE;
   const float sign = transposed ? -1.f : 1.f;
+#define TC_APPLY(PER_)                                                                                                                  \
+  rope_apply_kernel<T, INTER, VEC, PER_><<<(unsigned)blocks, 256, 0, st>>>((const T*)x, *xs, c, s, (T*)y, *ys, tokens, rows, heads, groups, \
+                                                                           items, r, sign)
   if (per == 4)
-    rope_apply_kernel<T, INTER, VEC, 4><<<(unsigned)blocks, 256, 0, st>>>((const T*)x, *xs, c, s, (T*)y, *ys, tokens, rows, heads, groups, items, r, sign);
+    TC_APPLY(4);
   else
-    rope_apply_kernel<T, INTER, VEC, 1><<<(unsigned)blocks, 256, 0, st>>>((const T*)x, *xs, c, s, (T*)y, *ys, tokens, rows, heads, groups, items, r, sign);
+    TC_APPLY(1);
+#undef TC_APPLY
+  return check_launch();
+}
+
+// New tokens of a cache: the heads of a token are those of its query, key and value in turn.  Queries and keys are turned, queries go to
+// the rows of the output, keys and values to their slots.
+template <typename T, bool INTER, bool VEC, int PER>
+__global__ __launch_bounds__(256) void append_kernel(const T* __restrict__ Q, tc_strides qs, const T* __restrict__ K, tc_strides ks,
+                                                     const T* __restrict__ V, tc_strides vs, const float* __restrict__ c,
+                                                     const float* __restrict__ s, const int32_t* __restrict__ pos,
+                                                     const int32_t* __restrict__ len, const int32_t* __restrict__ q_len, T* __restrict__ Qo,
+                                                     T* __restrict__ Kc, T* __restrict__ Vc, int32_t* __restrict__ slot_pos,
+                                                     float* __restrict__ weight, CachePlan pl, int groups, int items, int r) {
+  const RopeThread me = rope_thread(items, groups);
+  if (me.token >= (long long)pl.B * pl.T) return;
+  const int b = (int)(me.token / pl.T), t = (int)(me.token % pl.T);
+  typedef RopeItem<T, INTER, VEC> Item;
+  // (without tables nothing is turned: the item's own part of the row is copied)
+  const Item it(c + (c ? me.token * (r / 2) : 0), s + (s ? me.token * (r / 2) : 0), me.item, r, 1.f);
+  const int m = q_len ? clamp_len(q_len[b], pl.T) : pl.T, slot = clamp_len(len[b], pl.max_len) - m + t;
+  const bool live = t < m, stored = live && slot >= 0 && slot < pl.cap;
+  const T* from[PER];
+  T* to[PER];
+  typename Item::Data v[PER];
+#pragma unroll
+  for (int k = 0; k < PER; k++) {
+    const int h = me.head + k * groups;
+    from[k] = nullptr;
+    to[k] = nullptr;
+    if (h < pl.H) {
+      to[k] = Qo + (((size_t)b * pl.H + h) * pl.T + t) * pl.dh;
+      if (live) from[k] = Q + b * qs.batch + h * qs.head + t * qs.row;
+    } else if (h < pl.H + 2 * pl.Hk && stored) {
+      const bool key = h < pl.H + pl.Hk;
+      const int j = h - (key ? pl.H : pl.H + pl.Hk);
+      const tc_strides& st = key ? ks : vs;
+      from[k] = (key ? K : V) + b * st.batch + j * st.head + t * st.row;
+      const size_t at = ((size_t)b * pl.Hk + j) * pl.cap + slot;
+      to[k] = (key ? Kc : Vc) + at * pl.dh;
+      if (key && me.item == 0) {
+        slot_pos[at] = pos[me.token];
+        weight[at] = 0.f;
+      }
+    }
+    if (from[k]) it.load(from[k], v[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < PER; k++) {
+    if (!to[k]) continue;
+    if (!from[k])
+      v[k].a = v[k].b = uint4{0, 0, 0, 0};
+    else if (c && me.head + k * groups < pl.H + pl.Hk)
+      it.turn(v[k]);
+    it.store(to[k], v[k]);
+  }
+}
+
+template <typename T, bool INTER, bool VEC>
+static int append_launch(const CachePlan& pl, int r, const void* Q, const tc_strides* qs, const void* K, const tc_strides* ks, const void* V,
+                         const tc_strides* vs, const float* c, const float* s, const int32_t* pos, const int32_t* len, const int32_t* q_len,
+                         void* Qo, void* Kc, void* Vc, int32_t* slot_pos, float* weight, hipStream_t st) {
+  const int heads = pl.H + 2 * pl.Hk, items = rope_items(pl.dh, r, Vec16<T>::N, INTER, VEC);
+  const long long tokens = (long long)pl.B * pl.T;
+  const int per = rope_per(tokens, heads, items), groups = (heads + per - 1) / per;
+  const long long blocks = (tokens * groups * items + 255) / 256;
+  if (blocks > 0x7fffffffLL) return TC_ERR_SHAPE;
+#define TC_APPEND(PER_)                                                                                                                   \
+  append_kernel<T, INTER, VEC, PER_><<<(unsigned)blocks, 256, 0, st>>>((const T*)Q, *qs, (const T*)K, *ks, (const T*)V, *vs, c, s, pos, len, \
+                                                                       q_len, (T*)Qo, (T*)Kc, (T*)Vc, slot_pos, weight, pl, groups, items, r)
+  if (per == 4)
+    TC_APPEND(4);
+  else
+    TC_APPEND(1);
+#undef TC_APPEND
   return check_launch();
 }
 
 // F<T, INTER, VEC>(args) for the storage type, the layout and whether the rotated part falls into vectors.
-#define TC_ROPE_CALL(F, dtype, p, ...)                                                                             \
+#define TC_ROPE_CALL(F, dtype, r, layout, ...)                                                                     \
   [&]() -> int {                                                                                                   \
-    const bool inter = (p)->layout == TC_ROPE_INTERLEAVED;                                                         \
+    const bool inter = (layout) == TC_ROPE_INTERLEAVED;                                                            \
     auto by = [&](auto tag) -> int {                                                                               \
       typedef decltype(tag) T;                                                                                     \
-      if (rope_vec<T>(rope_dim(p), inter)) return inter ? F<T, true, true>(__VA_ARGS__) : F<T, false, true>(__VA_ARGS__); \
+      if (rope_vec<T>(r, inter)) return inter ? F<T, true, true>(__VA_ARGS__) : F<T, false, true>(__VA_ARGS__); \
       return inter ? F<T, true, false>(__VA_ARGS__) : F<T, false, false>(__VA_ARGS__);                             \
     };                                                                                                             \
     return (dtype) == TC_F32 ? by(0.f) : (dtype) == TC_BF16 ? by(uint16_t(0)) : by(f16_t{0});                      \
@@ -235,5 +312,28 @@ extern "C" int tc_rope_apply(const tc_rope* r, int32_t dtype, int32_t batch, int
   if (misaligned(x) || misaligned(cos) || misaligned(sin) || misaligned(y)) return TC_ERR_ALIGN;
   if (x == y && ((batch > 1 && xs->batch != ys->batch) || (n_heads > 1 && xs->head != ys->head) || (n_rows > 1 && xs->row != ys->row)))
     return TC_ERR_PARAM;
-  return TC_ROPE_CALL(rope_launch, dtype, r, r, batch, n_heads, n_rows, x, xs, cos, sin, y, ys, transposed, (hipStream_t)stream);
+  return TC_ROPE_CALL(rope_launch, dtype, rope_dim(r), r->layout, r, batch, n_heads, n_rows, x, xs, cos, sin, y, ys, transposed, (hipStream_t)stream);
+}
+
+extern "C" int tc_cache_append(const tc_cache* cache, const tc_rope* r, const void* Q, const tc_strides* qs, const void* K,
+                               const tc_strides* ks, const void* V, const tc_strides* vs, const float* cos, const float* sin,
+                               const int32_t* pos_ids, const int32_t* len, const int32_t* q_len, void* Q_out, void* K_cache, void* V_cache,
+                               int32_t* slot_pos, float* weight, void* stream) {
+  CachePlan pl;
+  int rc = make_cache_plan(cache, &pl);
+  if (rc != TC_OK) return rc;
+  if (r && (rc = check_rope(r)) != TC_OK) return rc;
+  if (r && r->head_dim != pl.dh) return TC_ERR_SHAPE;
+  if (pl.B == 0) return TC_OK;
+  if (!Q || !qs || !K || !ks || !V || !vs || !pos_ids || !len || !Q_out || !K_cache || !V_cache || !slot_pos || !weight) return TC_ERR_NULL;
+  if ((cos == nullptr) != (r == nullptr) || (sin == nullptr) != (r == nullptr)) return TC_ERR_NULL;
+  if (bad_strides(qs, pl.esize, pl.B, pl.H, pl.T, false) || bad_strides(ks, pl.esize, pl.B, pl.Hk, pl.T, false) ||
+      bad_strides(vs, pl.esize, pl.B, pl.Hk, pl.T, false))
+    return TC_ERR_SHAPE;
+  if (misaligned(Q) || misaligned(K) || misaligned(V) || misaligned(cos) || misaligned(sin) || misaligned(pos_ids) || misaligned(len) ||
+      misaligned(q_len) || misaligned(Q_out) || misaligned(K_cache) || misaligned(V_cache) || misaligned(slot_pos) || misaligned(weight))
+    return TC_ERR_ALIGN;
+  const int rd = r ? rope_dim(r) : pl.dh;
+  return TC_ROPE_CALL(append_launch, cache->dtype, rd, r ? r->layout : TC_ROPE_HALF, pl, rd, Q, qs, K, ks, V, vs, cos, sin, pos_ids, len,
+                      q_len, Q_out, K_cache, V_cache, slot_pos, weight, (hipStream_t)stream);
 }

@@ -28,7 +28,7 @@ def _fields(name):
 
 
 @needs_library
-@pytest.mark.parametrize("name", ["tc_rope", "tc_strides"])
+@pytest.mark.parametrize("name", ["tc_rope", "tc_strides", "tc_cache"])
 def test_structures_match_the_header(name):
     tc = _binding()
     kinds = {ctypes.c_int32: "int32_t", ctypes.c_int64: "int64_t", ctypes.c_float: "float"}
@@ -78,6 +78,103 @@ def test_rotary_entry_points_check_their_arguments():
         assert apply(ys=ctypes.byref(tc.tc_strides(*v))) == -2
         assert apply(xs=ctypes.byref(tc.tc_strides(*v))) == -4    # (got as far as the check of calls in place)
     assert apply(B=0, x=None) == apply(T=0, x=None) == 0
+
+
+CACHE = dict(batch=4, n_heads=8, n_kv_heads=2, head_dim=64, dtype=1, n_query=3, capacity=100, n_prefixes=2, prefix_len=10, budget=40, n_sink=4,
+             n_recent=8)
+
+
+def _calls(tc, **change):
+    """Every entry point on a cache, with arguments that name no memory; `change` replaces some of them."""
+    lib, F = tc.load_library(), FAKE
+    st = ctypes.byref(tc.tc_strides(1024, 64, 256))
+    a = dict(c=None, r=ctypes.byref(tc.make_rope(64)), Q=F, qs=st, K=F, ks=st, V=F, vs=st, cos=F, sin=F, pos=F, len=F, q_len=F, Qo=F, Kc=F, Vc=F,
+             sp=F, w=F, Ko=2 * F, Vo=2 * F, po=2 * F, wo=2 * F, cap=50, lo=2 * F, ws=F, bytes=1 << 40)
+    a.update(change)
+    v = lambda *names: [a[n] for n in names]  # noqa: E731
+    return {
+        "append": lambda: lib.tc_cache_append(*v("c", "r", "Q", "qs", "K", "ks", "V", "vs", "cos", "sin", "pos", "len", "q_len", "Qo", "Kc", "Vc", "sp", "w"), None),
+        "evict": lambda: lib.tc_cache_evict(*v("c", "len", "Kc", "Vc", "sp", "w", "Ko", "Vo", "po", "wo", "cap", "lo", "ws", "bytes"), None),
+    }
+
+
+@needs_library
+@pytest.mark.parametrize("kw,status", [
+    (dict(batch=-1), -2), (dict(batch=(1 << 16) + 2), -2), (dict(n_heads=0), -2), (dict(n_heads=2048), -2), (dict(n_kv_heads=3), -2),
+    (dict(n_kv_heads=0), -2), (dict(head_dim=96), -2), (dict(n_query=0), -2), (dict(n_query=(1 << 20) + 1), -2), (dict(capacity=0), -2),
+    (dict(capacity=(1 << 24) + 1), -2), (dict(max_len=101), -2), (dict(max_len=-1), -2), (dict(n_prefixes=3), -2), (dict(n_prefixes=-1), -2),
+    (dict(n_prefixes=0), -2), (dict(prefix_len=-1), -2), (dict(prefix_len=(1 << 24) + 1), -2), (dict(dtype=3), -3), (dict(softmax_scale=-1.0), -4),
+    (dict(softmax_scale=float("inf")), -4), (dict(softmax_scale=float("nan")), -4), (dict(budget=101), -4), (dict(budget=-1), -4),
+    (dict(n_sink=-1), -4), (dict(n_recent=-1), -4), (dict(n_sink=33), -4), (dict(n_sink=2 ** 31 - 1, n_recent=2 ** 31 - 1), -4),
+    (dict(batch=1 << 16, n_heads=1024, n_kv_heads=1024, n_query=1 << 20), -2)])
+def test_cache_parameters_out_of_range(kw, status):
+    tc = _binding()
+    c = tc.make_cache(**dict(CACHE, **kw))
+    assert tc.tc_cache_workspace_bytes(c) == 0
+    for name, call in _calls(tc, c=ctypes.byref(c)).items():
+        assert call() == status, name
+
+
+@needs_library
+def test_cache_entry_points_check_their_arguments():
+    tc = _binding()
+    c = tc.make_cache(**CACHE)
+    ok = ctypes.byref(c)
+    needed = {"append": ("Q", "qs", "K", "ks", "V", "vs", "cos", "sin", "pos", "len", "Qo", "Kc", "Vc", "sp", "w"),
+              "evict": ("len", "Kc", "Vc", "sp", "w", "Ko", "Vo", "po", "wo", "lo", "ws")}
+    for entry, names in needed.items():
+        for name in names:
+            assert _calls(tc, c=ok, **{name: None})[entry]() == -1, (entry, name)
+            if name not in ("qs", "ks", "vs"):
+                assert _calls(tc, c=ok, **{name: FAKE + 8})[entry]() == -6, (entry, name)
+        assert _calls(tc, c=None)[entry]() == -1
+        empty = ctypes.byref(tc.make_cache(**dict(CACHE, batch=0)))
+        assert _calls(tc, c=empty, **{name: None for name in names})[entry]() == 0
+    odd = ctypes.byref(tc.tc_strides(1024, 64, 4))
+    for name in ("qs", "ks", "vs"):
+        assert _calls(tc, c=ok, **{name: odd})["append"]() == -2
+    assert _calls(tc, c=ok, r=ctypes.byref(tc.make_rope(128)))["append"]() == -2
+    assert _calls(tc, c=ok, r=ctypes.byref(tc.make_rope(64, rot_dim=1)))["append"]() == -2
+    assert _calls(tc, c=ok, r=None)["append"]() == -1    # tables without what they are of
+    assert _calls(tc, c=ok, cap=39)["evict"]() == -2
+    assert _calls(tc, c=ok, bytes=tc.tc_cache_workspace_bytes(c) - 1)["evict"]() == -5
+    assert _calls(tc, c=ok, lo=FAKE)["evict"]() == -4     # the lengths are read while they are written
+    assert _calls(tc, c=ok, Ko=FAKE)["evict"]() == -4     # half in place
+    assert _calls(tc, c=ok, Ko=FAKE, Vo=FAKE, po=FAKE, wo=FAKE, cap=99)["evict"]() == -4
+    assert _calls(tc, c=ctypes.byref(tc.make_cache(**dict(CACHE, budget=0, n_sink=0, n_recent=0))))["evict"]() == -4
+
+
+@needs_library
+def test_cache_workspace_grows_with_the_cache_and_not_with_the_call():
+    tc = _binding()
+    size = lambda **kw: tc.tc_cache_workspace_bytes(tc.make_cache(**dict(CACHE, **kw)))  # noqa: E731
+    assert size() % 256 == 0
+    assert size(max_len=1) == size(max_len=50) == size(max_len=100) == size()
+    for name, values in (("batch", (2, 4, 64, 1000)), ("capacity", (40, 4096, 32768, 32769, 1 << 20)), ("budget", (12, 40, 100)),
+                         ("n_query", (1, 5, 17, 400)), ("prefix_len", (1, 100, 5000))):
+        sizes = [size(**{name: x}) for x in values]
+        assert sizes == sorted(sizes), name
+
+
+def test_oracle_appends_the_last_slots():
+    K, V, p, w = np.zeros((2, 5, 3)), np.zeros((2, 5, 3)), np.full((2, 5), -1), np.ones((2, 5))
+    k = np.arange(12.0).reshape(2, 2, 3)
+    orc.append(K, V, p, w, k, -k, [7, 9], 4)
+    assert np.array_equal(K[:, 2:4], k) and np.array_equal(V[:, 2:4], -k) and p.tolist() == [[-1, -1, 7, 9, -1]] * 2
+    assert w.tolist() == [[1, 1, 0, 0, 1]] * 2 and not K[:, [0, 1, 4]].any()
+    orc.append(K, V, p, w, k, -k, [7, 9], 6)    # the second one falls behind the cache
+    assert np.array_equal(K[:, 4], k[:, 0])
+
+
+def test_oracle_evicts_by_protection_weight_and_slot():
+    pos, w = [0, 1, 2, 3, 4, 5, 6, 7], [0.1, 5.0, 2.0, 2.0, float("nan"), 2.0, 0.3, 0.0]
+    # slot 0 and 7 are protected, 1 has the most, of 2, 3, 5 the first two stay
+    assert orc.evict(pos, w, 8, 5, 1, 1) == [0, 1, 2, 3, 7]
+    assert orc.evict(pos, w, 8, 4, 1, 1) == [0, 1, 2, 7]
+    assert orc.evict(pos, w, 8, 3, 0, 0) == [3, 1, 2]    # no one is protected: slot 3 comes to the freed slot 0
+    assert orc.evict(pos, w, 8, 2, 0, 1) == [7, 1]
+    assert orc.evict(pos, w, 5, 5, 0, 0) == [0, 1, 2, 3, 4] and orc.evict(pos, w, 0, 5, 0, 0) == []
+    assert orc.evict(pos, [0.0, -0.0] * 4, 8, 3, 0, 0) == [0, 1, 2]
 
 
 def test_oracle_turns_pairs_by_their_angle():

@@ -1,0 +1,192 @@
+"""Eviction against the oracle: which slots stay, where their rows go, what is left as it was."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def _tc():
+    from oracle import cache_oracle as orc
+    from paper_2503_10501_amd import binding as tc
+    tc.load_library()
+    return tc, orc
+
+
+def _weights(kind, shape, g):
+    w = torch.rand(shape, generator=g)
+    if kind == "ties":
+        w = (w * 4).floor()
+    if kind == "zero":
+        w = torch.where(w < 0.5, 0.0, -0.0)
+    if kind == "odd":
+        pick = torch.randint(0, 6, shape, generator=g)
+        for i, v in enumerate((float("nan"), float("inf"), -float("inf"), -1.0, 1e-40)):
+            w = torch.where(pick == i, v, w)
+    return w
+
+
+def _run(dtype, d, B, Hk, cap, lens, budget, sink=0, recent=0, kind="rand", in_place=True, out_cap=None, max_len=0, shuffled=False, seed=0,
+         positions=None):
+    tc, orc = _tc()
+    g, sd = torch.Generator().manual_seed(seed), DTYPES[dtype]
+    K, V = (torch.randn(B, Hk, cap, d, generator=g).to(sd).cuda() for _ in range(2))
+    sp = torch.arange(cap, dtype=torch.int32).expand(B, Hk, cap).clone()
+    if shuffled:
+        sp = torch.stack([torch.randperm(cap, generator=g) for _ in range(B * Hk)]).view(B, Hk, cap).to(torch.int32)
+    if positions is not None:
+        sp = positions.expand(B, Hk, cap).clone()
+    w = _weights(kind, (B, Hk, cap), g)
+    sp, w = sp.cuda(), w.cuda()
+    c = tc.make_cache(B, Hk, Hk, d, tc._DTYPES[dtype], 1, cap, max_len=max_len, budget=budget, n_sink=sink, n_recent=recent)
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    ws = torch.full((tc.tc_cache_workspace_bytes(c),), 0xff, dtype=torch.uint8, device="cuda")
+    left = torch.full((B,), -7, dtype=torch.int32, device="cuda")
+    src = [x.clone() for x in (K, V, sp, w)]
+    if in_place:
+        out = [K, V, sp, w]
+        tc.tc_cache_evict(c, n, K, V, sp, w, left, ws)
+    else:
+        oc = out_cap or budget
+        out = [torch.full((B, Hk, oc) + x.shape[3:], 3, dtype=x.dtype, device="cuda") for x in src]
+        tc.tc_cache_evict(c, n, K, V, sp, w, left, ws, K_out=out[0], V_out=out[1], pos_out=out[2], weight_out=out[3])
+    torch.cuda.synchronize()
+    most = max_len or cap
+    for b in range(B):
+        nb = min(max(lens[b], 0), most)
+        assert int(left[b]) == min(nb, budget)
+        for h in range(Hk):
+            source = orc.evict(src[2][b, h].tolist(), src[3][b, h].tolist(), nb, budget, sink, recent)
+            for x, o in zip(src, out):
+                was, got = (x if in_place else torch.full_like(o, 3))[b, h].clone(), o[b, h]
+                if source:
+                    was[:len(source)] = x[b, h][source]
+                bits = torch.int16 if got.element_size() == 2 else torch.int32
+                assert torch.equal(got.view(bits), was.view(bits)), (b, h)
+        if not in_place:
+            for x, y in zip(src, (K, V, sp, w)):
+                assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_types(dtype, d, in_place):
+    _run(dtype, d, 3, 2, 150, [150, 97, 40], 64, sink=3, recent=10, in_place=in_place, shuffled=True)
+
+
+@pytest.mark.parametrize("cap,budget", [(1, 1), (2, 1), (65, 64), (1024, 100), (1025, 1024), (1100, 1), (4096, 4000), (4097, 640), (9000, 8999),
+                                        (32768, 1000), (32769, 16384), (40000, 20001)])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_sizes(cap, budget, in_place):
+    # every variant of the selection, at its ends
+    _run("bf16", 64, 2, 1, cap, [cap, max(0, cap - 1)], budget, sink=budget // 5, recent=budget // 3, in_place=in_place)
+
+
+@pytest.mark.parametrize("kind", ["ties", "zero", "odd"])
+@pytest.mark.parametrize("cap", [300, 2000, 5000, 33000])
+def test_weights_that_tie_or_are_no_numbers(kind, cap):
+    _run("f16", 64, 2, 2, cap, [cap, cap - 37], cap // 3, recent=cap // 50, kind=kind, shuffled=True, seed=cap)
+
+
+@pytest.mark.parametrize("lens,max_len", [([0, 1, 63, 64, 65], 0), ([-5, 200, 64, 100, 99], 0), ([200, 80, 0, 64, 65], 80)])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_lengths_from_none_to_beyond(lens, max_len, in_place):
+    _run("bf16", 64, 5, 2, 100, lens, 64, recent=5, max_len=max_len, in_place=in_place, out_cap=70)
+
+
+def test_a_budget_that_nothing_passes_moves_nothing():
+    _run("bf16", 128, 2, 2, 50, [50, 31], 50, kind="odd")
+    _run("bf16", 128, 2, 2, 50, [40, 31], 45, kind="odd", max_len=45)
+
+
+@pytest.mark.parametrize("sink,recent", [(64, 0), (0, 64), (32, 32), (0, 0)])
+def test_protection_can_take_the_whole_budget(sink, recent):
+    _run("f32", 64, 2, 1, 200, [200, 129], 64, sink=sink, recent=recent, shuffled=True)
+
+
+def test_positions_that_repeat_or_lie_at_the_ends():
+    g = torch.Generator().manual_seed(3)
+    _run("bf16", 64, 2, 1, 120, [120, 90], 30, sink=4, recent=20, positions=torch.full((120,), 7, dtype=torch.int32))      # all protected
+    ends = torch.randint(-2 ** 31, 2 ** 31 - 1, (120,), generator=g).to(torch.int32)
+    ends[5], ends[11] = 2 ** 31 - 1, -2 ** 31
+    _run("bf16", 64, 2, 1, 120, [120, 90], 30, sink=0, recent=30, positions=ends)
+    _run("bf16", 64, 2, 1, 120, [120, 90], 30, sink=0, recent=30, positions=torch.full((120,), -2 ** 31, dtype=torch.int32))
+
+
+def test_a_stream_of_tokens_captured_and_replayed():
+    """One token in, one out: the captured step against the oracle run beside it, replay after replay with eager work between."""
+    tc, orc = _tc()
+    B, Hk, d, budget = 2, 2, 64, 12
+    cap = budget + 1
+    g = torch.Generator().manual_seed(11)
+    K, V = (torch.randn(B, Hk, cap, d, generator=g).cuda() for _ in range(2))
+    sp, w = torch.arange(cap, dtype=torch.int32).expand(B, Hk, cap).contiguous().cuda(), torch.rand(B, Hk, cap, generator=g).cuda()
+    c = tc.make_cache(B, Hk, Hk, d, tc.TC_F32, 1, cap, budget=budget, n_sink=2, n_recent=3)
+    ws = tc.new_cache_workspace(c)
+    n, left = torch.full((B,), cap, dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda")
+    new = torch.randn(B, Hk, 1, d, generator=g).cuda()
+    pos, q = torch.full((B, 1), cap - 1, dtype=torch.int32, device="cuda"), torch.empty(B, Hk, 1, d, device="cuda")
+
+    def step():
+        pos.add_(1)
+        tc.tc_cache_append(c, None, new, new, new, None, None, pos, n, q, K, V, sp, w)
+        tc.tc_cache_evict(c, n, K, V, sp, w, left, ws)
+
+    keep = [x.clone() for x in (K, V, sp, w, pos)]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for x, y in zip((K, V, sp, w, pos), keep):
+        x.copy_(y)
+    want = [x.cpu().double().numpy() for x in (K, V, sp, w)]
+    for it in range(6):
+        new.normal_()
+        fresh = new.cpu().double().numpy()
+        graph.replay()
+        torch.cuda.synchronize()
+        for b in range(B):
+            orc.append(*(x[b] for x in want), fresh[b], fresh[b], [cap + it], cap)
+            for h in range(Hk):
+                source = orc.evict(want[2][b, h], want[3][b, h], cap, budget, 2, 3)
+                for x in want:
+                    x[b, h, :budget] = x[b, h][source]
+        for x, y in zip((K, V, sp, w), want):
+            assert np.array_equal(x.cpu().double().numpy(), y), it
+        assert left.tolist() == [budget] * B
+
+
+def test_refusals():
+    tc, _ = _tc()
+    c = tc.make_cache(1, 1, 1, 64, tc.TC_BF16, 1, 8, budget=4)
+    sd = torch.bfloat16
+    t = dict(lens=torch.ones(1, dtype=torch.int32, device="cuda"), K_cache=torch.zeros(1, 1, 8, 64, dtype=sd, device="cuda"),
+             V_cache=torch.zeros(1, 1, 8, 64, dtype=sd, device="cuda"), slot_pos=torch.zeros(1, 1, 8, dtype=torch.int32, device="cuda"),
+             weight=torch.zeros(1, 1, 8, device="cuda"), len_out=torch.zeros(1, dtype=torch.int32, device="cuda"), ws=tc.new_cache_workspace(c))
+    out = dict(K_out=torch.zeros(1, 1, 4, 64, dtype=sd, device="cuda"), V_out=torch.zeros(1, 1, 4, 64, dtype=sd, device="cuda"),
+               pos_out=torch.zeros(1, 1, 4, dtype=torch.int32, device="cuda"), weight_out=torch.zeros(1, 1, 4, device="cuda"))
+    tc.tc_cache_evict(c, **t)
+    tc.tc_cache_evict(c, **t, **out)
+    for name in dict(t, **out):
+        bad = dict(t, **out)
+        for x in (bad[name].cpu(), bad[name].double()):
+            with pytest.raises(ValueError):
+                tc.tc_cache_evict(c, **dict(bad, **{name: x}))
+        if name in out:
+            with pytest.raises(ValueError):
+                tc.tc_cache_evict(c, **{k: v for k, v in bad.items() if k != name})
+    for kw, status in ((dict(ws=t["ws"][:16]), -5), (dict(len_out=t["lens"]), -4)):
+        with pytest.raises(tc.TokenCarveError) as e:
+            tc.tc_cache_evict(c, **dict(t, **kw))
+        assert e.value.status == status
+    with pytest.raises(tc.TokenCarveError) as e:   # no room for what stays
+        tc.tc_cache_evict(c, **t, **{k: v[:, :, :3].contiguous() for k, v in out.items()})
+    assert e.value.status == -2
+    with pytest.raises(tc.TokenCarveError):
+        tc.tc_cache_evict(tc.make_cache(1, 1, 1, 64, tc.TC_BF16, 1, 8), **t)
