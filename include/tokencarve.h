@@ -399,6 +399,22 @@ TC_API int tc_cache_append(const tc_cache* c, const tc_rope* r, const void* Q, c
                            float* weight, void* stream);
 
 /*
+ * Attention of the call's tokens over the prefix that their sequences share and over their own cache: row t < q_len[b] of a head sees
+ * every key of the prefix and the slots 0 .. len[b] - q_len[b] + t (its own among them, no later one).
+ *     O[b, t, h*d_h + e] = sum_k p_k V_k[e],  p = softmax over the keys that the row sees of Q K^T * scale, rounded once
+ *     weight[b, h_kv, j] += sum over the rows t < q_len[b] of the heads that share h_kv of p_j       (slots, not the prefix)
+ *   Q         [B, H, T, d_h]            (Q_out of tc_cache_append)
+ *   K_prefix, V_prefix [n_prefixes, H_kv, P, d_h]  both NULL where P = 0.  A prefix is read once for all rows of its sequences
+ *   K_cache, V_cache [B, H_kv, capacity, d_h]      slots behind len[b] are not looked at: they may hold anything
+ *   O         [B, T, H*d_h]             rows t >= q_len[b], and rows that see no key, are zero
+ *   weight    [B, H_kv, capacity] float, read and written, sums in a fixed order; NULL: not wanted
+ * What a row does not see has no influence on it, infinities and NaN included.  No two tensors overlap.
+ */
+TC_API int tc_cache_attention(const tc_cache* c, const void* Q, const void* K_prefix, const void* V_prefix, const void* K_cache,
+                              const void* V_cache, const int32_t* len, const int32_t* q_len, void* O, float* weight, void* ws,
+                              size_t ws_bytes, void* stream);
+
+/*
  * Eviction: of every sequence and key/value head the `budget` best slots stay in use.  A slot whose position is below n_sink or above
  * newest - n_recent (newest: the largest position in use) comes before the others, these come by weight, largest first (NaN last), equal
  * ones by slot, lowest first.  Slots 0 .. budget-1 that stay keep what they hold; the others that stay go, in ascending order, to the

@@ -24,7 +24,7 @@ TC_ROPE_PLAIN, TC_ROPE_LINEAR, TC_ROPE_BASE, TC_ROPE_BANDS = 0, 1, 2, 3
 SYMBOLS = ("tc_workspace_bytes", "tc_status_string", "tc_attn_output", "tc_ipgs_score", "tc_select_topk",
            "tc_merge", "tc_merge_noalloc", "tc_similarity", "tc_compress", "tc_profile_compress", "tc_probe_rates", "tc_info_rank",
            "tc_assemble_sequence", "tc_kv_cache_fraction", "tc_rope_tables", "tc_rope_apply",
-           "tc_cache_workspace_bytes", "tc_cache_append", "tc_cache_evict")
+           "tc_cache_workspace_bytes", "tc_cache_append", "tc_cache_attention", "tc_cache_evict")
 PROF_KINDS = ("attn", "attn_reduce", "gram", "jacobi_init", "jacobi_solve", "jacobi_update", "jacobi_update_u", "jacobi_sweep_end",
               "sigma", "ics", "combine", "topk", "rownorm", "sim", "assign", "average", "tridiag", "bisect", "twisted",
               "backtransform", "tridiag_update")
@@ -134,6 +134,7 @@ def load_library():
     cp = ctypes.POINTER(tc_cache)
     lib.tc_cache_workspace_bytes.argtypes = [cp]
     lib.tc_cache_append.argtypes = [cp, rp, vp, sp, vp, sp, vp, sp] + [vp] * 11
+    lib.tc_cache_attention.argtypes = [cp] + [vp] * 10 + [sz, vp]
     lib.tc_cache_evict.argtypes = [cp] + [vp] * 9 + [i32, vp, vp, sz, vp]
     for name in SYMBOLS[2:]:
         getattr(lib, name).restype = ctypes.c_int
@@ -400,6 +401,21 @@ def tc_cache_append(c, r, Q, K, V, cos, sin, pos_ids, lens, Q_out, K_cache, V_ca
     with _on(dev, stream) as st:
         _check(load_library().tc_cache_append(ctypes.byref(c), None if r is None else ctypes.byref(r), q, qs, k, ks, v, vs, co, si, pos, ln,
                                               ql, out, kc, vc, sp, w, st))
+
+
+def tc_cache_attention(c, Q, K_cache, V_cache, lens, O, ws, K_prefix=None, V_prefix=None, weight=None, q_len=None, stream=None):
+    dev, sd = _device("Q", Q), storage_dtype(c)
+    B, H, Hk, T, d = c.batch, c.n_heads, c.n_kv_heads, c.n_query, c.head_dim
+    q = _whole("Q", Q, (B, H, T, d), sd, dev)
+    prefix = (c.n_prefixes, Hk, c.prefix_len, d)
+    if c.prefix_len > 0 and (K_prefix is None or V_prefix is None):
+        raise ValueError("K_prefix, V_prefix: expected shape %s" % (prefix,))
+    kp, vp = _whole("K_prefix", K_prefix, prefix, sd, dev), _whole("V_prefix", V_prefix, prefix, sd, dev)
+    kc, vc, ln, ql = _cached(c, K_cache, V_cache, lens, q_len, dev)
+    o, w = _whole("O", O, (B, T, H * d), sd, dev), _whole("weight", weight, (B, Hk, c.capacity), torch.float32, dev)
+    work = _whole("ws", ws, ws.shape, torch.uint8, dev)
+    with _on(dev, stream) as st:
+        _check(load_library().tc_cache_attention(ctypes.byref(c), q, kp, vp, kc, vc, ln, ql, o, w, work, ws.numel(), st))
 
 
 def tc_cache_evict(c, lens, K_cache, V_cache, slot_pos, weight, len_out, ws, K_out=None, V_out=None, pos_out=None, weight_out=None,

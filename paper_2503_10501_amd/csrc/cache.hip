@@ -25,7 +25,8 @@ int make_cache_plan(const tc_cache* c, CachePlan* plan) {
   q.scale = c->softmax_scale > 0.f ? c->softmax_scale : 1.0f / std::sqrt((float)q.dh);
   if ((long long)q.B * q.H * q.T > (1LL << 31) - 1) return TC_ERR_SHAPE;  // rows are counted in 32 bits
   q.budget = c->budget; q.sink = c->n_sink; q.recent = c->n_recent;
-  q.total = align256(evict_bytes(q) + 256);
+  const size_t a = attention_bytes(q), e = evict_bytes(q);
+  q.total = align256((a > e ? a : e) + 256);
   return TC_OK;
 }
 

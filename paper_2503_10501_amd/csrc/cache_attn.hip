@@ -1,0 +1,507 @@
+// Attention of a call's tokens over a shared prefix and their own cache, and the attention that slots gather.
+//
+// The rows of queries of a sequence that read one key/value head, G heads of T rows, lie side by side in Q and are one matrix: row r = g T + t.
+// Scores are formed transposed, S^T = K Q^T, on the matrix cores, so that a lane has one row's scores and the probabilities are the operand of
+// O^T += V^T P^T as they lie; one pass over the keys with the running maximum and sum of the softmax in base 2.  Keys are split
+// between workgroups where rows are few; what these find, (maximum, sum, O), is joined by a second kernel.
+#include <cmath>
+
+#include "cache_internal.h"
+
+namespace tc {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bfrag;
+typedef __attribute__((ext_vector_type(8))) _Float16 hfrag;
+typedef __attribute__((ext_vector_type(4))) short short4v;
+typedef __attribute__((ext_vector_type(4))) float f4;
+typedef __attribute__((ext_vector_type(4))) unsigned int u4;
+typedef __attribute__((ext_vector_type(2))) unsigned int u2;
+typedef __attribute__((ext_vector_type(2))) float f2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf2;
+typedef __attribute__((ext_vector_type(2))) _Float16 h2;
+
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }  // (results below the smallest normal number: 0)
+
+// Products of 16 x 16 tiles over 32 elements: lane i + 16 g holds elements 8 g .. 8 g + 7 of row i of A and of column i of B, and gets rows
+// 4 g .. 4 g + 3 of column i of the product.  For float32 in eight steps of four elements.
+template <typename T> struct Mma;
+template <> struct Mma<uint16_t> {
+  typedef union { u4 u; uint32_t w[4]; bfrag v; short4v h[2]; } frag;
+  static constexpr bool WIDE = true;  // exponents of float32: sums of unscaled probabilities times values could pass its range
+  __device__ static inline f4 mul(const frag& a, const frag& b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0); }
+  // two floats as packed 16-bit heads, and what this rounding leaves
+  __device__ static inline uint32_t head(float x, float y) {
+    union { bf2 v; uint32_t w; } h;
+    h.v = __builtin_convertvector(f2{x, y}, bf2);
+    return h.w;
+  }
+  __device__ static inline void split(float x, float y, uint32_t& h, uint32_t& r) {
+    h = head(x, y);
+    r = head(x - __uint_as_float(h << 16), y - __uint_as_float(h & 0xffff0000u));
+  }
+};
+template <> struct Mma<f16_t> {
+  typedef union { u4 u; uint32_t w[4]; hfrag v; short4v h[2]; } frag;
+  static constexpr bool WIDE = false;
+  __device__ static inline f4 mul(const frag& a, const frag& b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, b.v, c, 0, 0, 0); }
+  __device__ static inline uint32_t head(float x, float y) {
+    union { h2 v; uint32_t w; } h;
+    h.v = __builtin_convertvector(f2{x, y}, h2);
+    return h.w;
+  }
+  __device__ static inline void split(float x, float y, uint32_t& h, uint32_t& r) {
+    union { h2 v; uint32_t w; } q;
+    q.w = h = head(x, y);
+    r = head(x - (float)q.v[0], y - (float)q.v[1]);
+  }
+};
+template <> struct Mma<float> {
+  typedef union { u4 u[2]; float f[8]; } frag;
+  static constexpr bool WIDE = true;
+  __device__ static inline f4 mul(const frag& a, const frag& b, f4 c) {
+#pragma unroll
+    for (int j = 0; j < 8; j++) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.f[j], b.f[j], c, 0, 0, 0);
+    return c;
+  }
+};
+// elements 8 at .. 8 at + 7 of a row of 16-byte vectors
+template <typename T>
+__device__ inline typename Mma<T>::frag frag_of(const u4* row, int at) {
+  typename Mma<T>::frag f;
+  if constexpr (sizeof(T) == 4) {
+    f.u[0] = row[2 * at];
+    f.u[1] = row[2 * at + 1];
+  } else {
+    f.u = row[at];
+  }
+  return f;
+}
+
+// The larger of a value and that of the lanes 16, 32 and 48 further on: the lanes that share a column of a product.
+__device__ inline float col_max(float x) {
+  const u2 a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const u2 b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ inline float col_sum(float x) {
+  const u2 a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const u2 b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// LDS that only one wavefront uses: its accesses are executed in order, and the compiler keeps that order here.
+__device__ inline void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// What the kernels are told.
+struct AttnArgs {
+  const void *Q, *Kp, *Vp, *Kc, *Vc;
+  const int32_t *len, *q_len;
+  void* O;
+  float* weight;
+  f2* ml;       // [part][row]: running maximum (base 2, with the offset below) and sum
+  float* part;  // [part][row][d_h]
+  float* lse;   // [row]: base-2 logarithm of the sum of all probabilities' numerators; +inf: the row gives nothing to anyone
+  int H, Hk, G, T, R, cap, max_len, each, P;
+  int rows;     // all rows: B H T
+  int splits;   // parts of the keys
+  float scale2; // scale log2(e)
+  float offset; // probabilities are formed as 2^(s - m - offset), so that sums of them times values stay within float32
+};
+
+// Row r of a sequence: what it sees of the cache.  Rows behind the last token see what that one sees; nothing of them is kept.
+__device__ inline int seen(const AttnArgs& a, int r, int n, int m) {
+  const int t = min(r % a.T, m - 1);
+  return clamp_len(n - m + t + 1, n);
+}
+
+// Where row `row` (of all rows) of the output lies.
+__device__ inline size_t out_row(const AttnArgs& a, int row, int dh) {
+  const int t = row % a.T, h = row / a.T % a.H, b = row / a.T / a.H;
+  return (((size_t)b * a.T + t) * a.H + h) * dh;
+}
+
+template <typename T>
+__device__ inline bool not_finite(T v) {
+  if constexpr (sizeof(T) == 4) return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u;
+  else if constexpr (Mma<T>::WIDE) return (v & 0x7f80u) == 0x7f80u;
+  else return (__builtin_bit_cast(uint16_t, v) & 0x7c00u) == 0x7c00u;
+}
+template <typename T>
+__device__ inline bool any_not_finite(const u4& w) {
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const uint32_t x = w[i];
+    if constexpr (sizeof(T) == 4) {
+      bad |= (x & 0x7f800000u) == 0x7f800000u;
+    } else {
+      constexpr uint32_t E = Mma<T>::WIDE ? 0x7f80u : 0x7c00u;
+      bad |= (x & E) == E || (x & E << 16) == E << 16;
+    }
+  }
+  return bad;
+}
+
+// ---- few rows: one workgroup has 16 rows, its four wavefronts share the keys, 32 at a time, without waiting for one another ----
+
+constexpr int FK = 32;  // keys of a wavefront's tile
+template <typename T, int DH>
+struct FewShape {
+  static constexpr int ES = sizeof(T), VEC = DH * ES / 16;             // 16-byte vectors of a row
+  static constexpr int KLD = DH * ES + 16, VLD = DH * ES + (ES == 2 ? 32 : 16);  // rows in LDS: lanes of a product's operand meet other banks
+  static constexpr int NV = FK * VEC / 64;                             // vectors of a lane
+  static constexpr int WAVE = FK * (KLD + VLD), LDS = 4 * WAVE;
+  static_assert(16 * (DH + 4) * 4 <= WAVE, "the partial output takes the place of the tiles");
+};
+
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void few_kernel(AttnArgs a, int tiles) {
+  typedef FewShape<T, DH> S;
+  typedef Mma<T> M;
+  typedef typename M::frag frag;
+  constexpr int ES = S::ES, VEC = S::VEC, NV = S::NV, DT = DH / 16;
+  extern __shared__ __attribute__((aligned(16))) unsigned char cache_smem[];
+  __shared__ float wave_m[4][16], wave_l[4][16], row_sum[16];  // row_sum: infinite for a row whose output is zero
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
+  const unsigned item = blockIdx.x;
+  const int split = item % a.splits, tile = item / a.splits % tiles;
+  const unsigned bh = item / a.splits / tiles;
+  const int b = bh / a.Hk, hk = bh % a.Hk;
+  const int n = clamp_len(a.len[b], a.max_len), m = a.q_len ? clamp_len(a.q_len[b], a.T) : a.T;
+  const int r = tile * 16 + i, row = bh * a.R + r;  // this lane's row of queries
+  const bool live = r < a.R && r % a.T < m;
+  const int end = m > 0 ? seen(a, min(r, a.R - 1), n, m) : 0;
+  int most = end, least = end;
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) {
+    most = max(most, __shfl_xor(most, o, 64));
+    least = min(least, __shfl_xor(least, o, 64));
+  }
+  most = __builtin_amdgcn_readfirstlane(most);
+  least = __builtin_amdgcn_readfirstlane(least);
+  // tiles of the prefix, then of the cache; this workgroup's share of them, dealt to its wavefronts in turn
+  const int np = m > 0 ? (a.P + FK - 1) / FK : 0, all = np + (most + FK - 1) / FK;
+  const int t0 = (int)((long long)all * split / a.splits), t1 = (int)((long long)all * (split + 1) / a.splits);
+
+  const size_t head = (size_t)bh * a.cap, phead = a.P > 0 ? ((size_t)(b / a.each) * a.Hk + hk) * a.P : 0;
+  unsigned char* Ks = cache_smem + wave * S::WAVE;
+  unsigned char* Vs = Ks + FK * S::KLD;
+  u4 kr[NV], vr[NV];
+  // a tile comes through registers: rows behind the last key are read as the last one, and their values as zero
+  auto fetch = [&](int t) {
+    const bool pre = t < np;
+    const int k0 = (pre ? t : t - np) * FK, last = (pre ? a.P : most) - 1;
+    const u4* K = reinterpret_cast<const u4*>(static_cast<const T*>(pre ? a.Kp : a.Kc) + (pre ? phead : head) * DH);
+    const u4* V = reinterpret_cast<const u4*>(static_cast<const T*>(pre ? a.Vp : a.Vc) + (pre ? phead : head) * DH);
+#pragma unroll
+    for (int j = 0; j < NV; j++) {
+      const int at = lane + 64 * j, key = k0 + at / VEC;
+      kr[j] = K[(size_t)min(key, last) * VEC + at % VEC];
+      const u4 v = V[(size_t)min(key, last) * VEC + at % VEC];
+      vr[j] = key <= last ? v : u4{0, 0, 0, 0};
+    }
+  };
+
+  frag q[DH / 32];
+  {
+    const u4* Qr = reinterpret_cast<const u4*>(static_cast<const T*>(a.Q) + (size_t)(bh * a.R + min(r, a.R - 1)) * DH);
+#pragma unroll
+    for (int s = 0; s < DH / 32; s++) q[s] = frag_of<T>(Qr, 4 * s + g);
+  }
+  f4 o[DT];
+#pragma unroll
+  for (int d = 0; d < DT; d++) o[d] = f4{0.f, 0.f, 0.f, 0.f};
+  float mx = -INFINITY, sum = 0.f;
+
+  int t = t0 + wave;
+  if (t < t1) fetch(t);
+  for (; t < t1; t += 4) {
+    const bool pre = t < np;
+    const int k0 = (pre ? t : t - np) * FK, last = pre ? a.P : most;
+    const bool masked = k0 + FK > (pre ? a.P : least);  // some row does not see some key
+    bool odd = false;                                    // a value that is not finite where rows differ in what they see
+    if (masked) {
+#pragma unroll
+      for (int j = 0; j < NV; j++) odd |= any_not_finite<T>(vr[j]);
+    }
+    odd = __ballot(odd) != 0;
+#pragma unroll
+    for (int j = 0; j < NV; j++) {
+      const int at = lane + 64 * j, key = at / VEC, c = at % VEC;
+      *reinterpret_cast<u4*>(Ks + key * S::KLD + c * 16) = kr[j];
+      *reinterpret_cast<u4*>(Vs + key * S::VLD + c * 16) = vr[j];
+    }
+    if (t + 4 < t1) fetch(t + 4);
+    wave_lds_order();
+
+    f4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+    for (int c = 0; c < DH / 32; c++)
+#pragma unroll
+      for (int u = 0; u < 2; u++)
+        s[u] = M::mul(frag_of<T>(reinterpret_cast<const u4*>(Ks + (16 * u + i) * S::KLD), 4 * c + g), q[c], s[u]);
+    float top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < 2; u++)
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const int key = k0 + 16 * u + 4 * g + e;
+        s[u][e] = !masked || key < (pre ? last : end) ? s[u][e] * a.scale2 : -INFINITY;
+        top = fmaxf(top, s[u][e]);
+      }
+    top = fmaxf(mx, col_max(top));
+    const float ref = top == -INFINITY ? 0.f : top + a.offset;
+    if (__ballot(top > mx)) {
+      const float f = exp2_fast(mx + a.offset - ref);
+      sum *= f;
+#pragma unroll
+      for (int d = 0; d < DT; d++) o[d] *= f;
+    }
+    mx = top;
+    float p[8];
+#pragma unroll
+    for (int u = 0; u < 2; u++)
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        p[4 * u + e] = exp2_fast(s[u][e] - ref);
+        sum += p[4 * u + e];
+      }
+    // element j of a lane's operands is key 4 g + j, from j = 4 on key 16 + 4 g + j - 4
+    frag ph, pr;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int j = 0; j < 8; j++) ph.f[j] = p[j];
+    } else {
+      // probabilities enter as a 16-bit head and the remainder: O is accurate to its own rounding
+#pragma unroll
+      for (int j = 0; j < 4; j++) M::split(p[2 * j], p[2 * j + 1], ph.w[j], pr.w[j]);
+    }
+#pragma unroll
+    for (int d = 0; d < DT; d++) {
+      frag v;
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+          v.f[j] = *reinterpret_cast<const float*>(Vs + (4 * g + (j & 3) + 16 * (j >> 2)) * S::VLD + (16 * d + i) * 4);
+      } else {
+        // the transposing read: 16 lanes name four rows of 16 elements and get a column each
+#pragma unroll
+        for (int u = 0; u < 2; u++) {
+          unsigned char* at = Vs + (16 * u + 4 * g + i / 4) * S::VLD + (16 * d + 4 * (i % 4)) * 2;
+          v.h[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)at);
+        }
+      }
+      if (odd) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+          for (int j = 0; j < 8; j++) v.f[j] = not_finite(v.f[j]) ? 0.f : v.f[j];
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; j++) {
+            const uint32_t w = v.w[j];
+            v.w[j] = (not_finite<T>(__builtin_bit_cast(T, (uint16_t)w)) ? 0 : w & 0xffffu) |
+                     (not_finite<T>(__builtin_bit_cast(T, (uint16_t)(w >> 16))) ? 0 : w & 0xffff0000u);
+          }
+        }
+      }
+      o[d] = M::mul(v, ph, o[d]);
+      if constexpr (sizeof(T) == 2) o[d] = M::mul(v, pr, o[d]);
+    }
+    if (odd) {  // values that are not finite reach the rows that see them, and no other
+      for (int k = 0; k < FK; k++) {
+        if (k0 + k >= (pre ? last : end)) continue;
+#pragma unroll
+        for (int d = 0; d < DT; d++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) {
+            const T v = *reinterpret_cast<const T*>(Vs + k * S::VLD + (16 * d + 4 * g + e) * ES);
+            if (not_finite(v)) o[d][e] += Vec16<T>::one(v);
+          }
+      }
+    }
+    wave_lds_order();
+  }
+  sum = col_sum(sum);
+
+  // the four wavefronts' parts
+  if (g == 0) {
+    wave_m[wave][i] = mx;
+    wave_l[wave][i] = sum;
+  }
+  __syncthreads();
+  float top = -INFINITY, total = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; w++) top = fmaxf(top, wave_m[w][i]);
+  const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+  for (int w = 0; w < 4; w++) total += wave_l[w][i] * exp2_fast(wave_m[w][i] - ref);
+  const float f = exp2_fast(mx - ref);
+  float* part = reinterpret_cast<float*>(cache_smem + wave * S::WAVE);
+#pragma unroll
+  for (int d = 0; d < DT; d++) *reinterpret_cast<f4*>(part + i * (DH + 4) + 16 * d + 4 * g) = o[d] * f;
+  if (threadIdx.x < 16 && r < a.R) {  // (wavefront 0, lane i: row i)
+    if (a.splits > 1) a.ml[(size_t)split * a.rows + row] = f2{top == -INFINITY ? top : top + a.offset, total};
+    else if (a.lse) a.lse[row] = live ? ref + a.offset + log2f(total) : INFINITY;
+    row_sum[i] = live && a.P + end > 0 ? total : INFINITY;
+  }
+  __syncthreads();
+  if (a.splits > 1 && t0 >= t1) return;
+  for (int at = threadIdx.x; at < 16 * DH / 4; at += 256) {
+    const int rr = at / (DH / 4), c = at % (DH / 4);
+    if (tile * 16 + rr >= a.R) continue;
+    f4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; w++) v += *reinterpret_cast<const f4*>(cache_smem + w * S::WAVE + (rr * (DH + 4) + 4 * c) * 4);
+    const int to = bh * a.R + tile * 16 + rr;
+    if (a.splits > 1) {
+      *reinterpret_cast<f4*>(a.part + ((size_t)split * a.rows + to) * DH + 4 * c) = v;
+    } else {
+      v = row_sum[rr] < INFINITY || row_sum[rr] != row_sum[rr] ? v / row_sum[rr] : f4{0.f, 0.f, 0.f, 0.f};
+      T* out = static_cast<T*>(a.O) + out_row(a, to, DH) + 4 * c;
+#pragma unroll
+      for (int e = 0; e < 4; e++) out[e] = Vec16<T>::round(v[e]);
+    }
+  }
+}
+
+// The parts of a row joined: one wavefront per row.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
+  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (row >= a.rows) return;
+  const int b = row / a.T / a.H, t = row % a.T;
+  const int n = clamp_len(a.len[b], a.max_len), m = a.q_len ? clamp_len(a.q_len[b], a.T) : a.T;
+  const bool live = t < m && a.P + clamp_len(n - m + t + 1, n) > 0;
+  float top = -INFINITY;
+  for (int s = 0; s < a.splits; s++) top = fmaxf(top, a.ml[(size_t)s * a.rows + row][0]);
+  const float ref = top == -INFINITY ? 0.f : top;
+  float total = 0.f, v[DH / 64];
+#pragma unroll
+  for (int e = 0; e < DH / 64; e++) v[e] = 0.f;
+  for (int s = 0; s < a.splits; s++) {
+    const f2 x = a.ml[(size_t)s * a.rows + row];
+    if (x[0] == -INFINITY && x[1] == 0.f) continue;  // saw nothing: its part is not written
+    const float f = exp2_fast(x[0] - ref);
+    total += f * x[1];
+#pragma unroll
+    for (int e = 0; e < DH / 64; e++) v[e] += f * a.part[((size_t)s * a.rows + row) * DH + 64 * e + lane];
+  }
+  T* out = static_cast<T*>(a.O) + out_row(a, row, DH) + lane;
+#pragma unroll
+  for (int e = 0; e < DH / 64; e++) out[64 * e] = Vec16<T>::round(live ? v[e] / total : 0.f);
+  if (a.lse && lane == 0) a.lse[row] = live ? ref + log2f(total) : INFINITY;
+}
+
+// What slots gather: 16 keys per wavefront, kept in registers; the rows of queries pass by, 16 at a time.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void gather_kernel(AttnArgs a, int chunks) {
+  typedef Mma<T> M;
+  typedef typename M::frag frag;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+  const unsigned bh = blockIdx.x / chunks;
+  const int b = bh / a.Hk, k0 = (int)(blockIdx.x % chunks) * 64 + wave * 16;
+  const int n = clamp_len(a.len[b], a.max_len), m = a.q_len ? clamp_len(a.q_len[b], a.T) : a.T;
+  if (k0 >= n || m == 0) return;
+  frag k[DH / 32];
+  const u4* Kr = reinterpret_cast<const u4*>(static_cast<const T*>(a.Kc) + ((size_t)bh * a.cap + min(k0 + i, n - 1)) * DH);
+#pragma unroll
+  for (int s = 0; s < DH / 32; s++) k[s] = frag_of<T>(Kr, 4 * s + g);
+  f4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int r0 = 0; r0 < a.R; r0 += 16) {
+    const int r = min(r0 + i, a.R - 1);
+    const size_t row = (size_t)bh * a.R + r;
+    const u4* Qr = reinterpret_cast<const u4*>(static_cast<const T*>(a.Q) + row * DH);
+    f4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < DH / 32; c++) s = M::mul(k[c], frag_of<T>(Qr, 4 * c + g), s);
+    const float lse = r0 + i < a.R ? a.lse[row] : INFINITY;
+    const int end = seen(a, r, n, m);
+#pragma unroll
+    for (int e = 0; e < 4; e++) acc[e] += lse < INFINITY && k0 + 4 * g + e < end ? exp2_fast(s[e] * a.scale2 - lse) : 0.f;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; e++)
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) acc[e] += __shfl_xor(acc[e], o, 64);
+  if (i < 4 && k0 + 4 * g + i < n) {
+    const float x = i == 0 ? acc[0] : i == 1 ? acc[1] : i == 2 ? acc[2] : acc[3];
+    a.weight[(size_t)bh * a.cap + k0 + 4 * g + i] += x;
+  }
+}
+
+// Parts of the keys: enough workgroups for the chip, and no more than there are tiles for the wavefronts.
+static int few_splits(const CachePlan& pl) {
+  const long long items = (long long)pl.B * pl.Hk * ((pl.R + 15) / 16);
+  const int tiles = (pl.P + FK - 1) / FK + (pl.max_len + FK - 1) / FK;
+  long long s = items > 0 ? (1024 + items - 1) / items : 1;
+  if (s > (tiles + 3) / 4) s = (tiles + 3) / 4;
+  return s < 1 ? 1 : (int)s;
+}
+
+// Rows of parts: at most 1024 + items workgroups of 16 rows where keys are split, which they are below 1024 items.
+static size_t part_rows(const CachePlan& pl) {
+  const long long items = (long long)pl.B * pl.Hk * ((pl.R + 15) / 16);
+  return (size_t)(1024 + (items < 1024 ? items : 1024)) * 16;
+}
+size_t attention_bytes(const CachePlan& pl) {
+  return align256((size_t)pl.B * pl.H * pl.T * 4) + align256(part_rows(pl) * 8) + part_rows(pl) * pl.dh * 4;
+}
+
+template <typename T, int DH>
+static int attention_launch(const CachePlan& pl, AttnArgs a, hipStream_t st) {
+  typedef FewShape<T, DH> S;
+  const int tiles = (pl.R + 15) / 16;
+  a.splits = few_splits(pl);
+  const long long grid = (long long)pl.B * pl.Hk * tiles * a.splits, chunks = (pl.max_len + 63) / 64;
+  if (grid > 0x7fffffffLL || (a.weight && chunks * pl.B * pl.Hk > 0x7fffffffLL)) return TC_ERR_SHAPE;
+  if (S::LDS + 1024 > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(few_kernel<T, DH>),
+                                                       hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS) != hipSuccess)
+    return TC_ERR_HIP;
+  few_kernel<T, DH><<<(unsigned)grid, 256, S::LDS, st>>>(a, tiles);
+  if (a.splits > 1) join_kernel<T, DH><<<(a.rows + 3) / 4, 256, 0, st>>>(a);
+  if (a.weight) gather_kernel<T, DH><<<(unsigned)(chunks * pl.B * pl.Hk), 256, 0, st>>>(a, (int)chunks);
+  return check_launch();
+}
+
+}  // namespace tc
+
+using namespace tc;
+
+extern "C" int tc_cache_attention(const tc_cache* c, const void* Q, const void* K_prefix, const void* V_prefix, const void* K_cache,
+                                  const void* V_cache, const int32_t* len, const int32_t* q_len, void* O, float* weight, void* ws,
+                                  size_t ws_bytes, void* stream) {
+  CachePlan pl;
+  int rc = make_cache_plan(c, &pl);
+  if (rc != TC_OK) return rc;
+  if (pl.B == 0) return TC_OK;
+  if (!Q || !K_cache || !V_cache || !len || !O || (pl.P > 0 && (!K_prefix || !V_prefix))) return TC_ERR_NULL;
+  if (misaligned(Q) || misaligned(K_prefix) || misaligned(V_prefix) || misaligned(K_cache) || misaligned(V_cache) || misaligned(len) ||
+      misaligned(q_len) || misaligned(O) || misaligned(weight))
+    return TC_ERR_ALIGN;
+  if ((rc = check_cache_ws(pl, ws, ws_bytes)) != TC_OK) return rc;
+  AttnArgs a = {};
+  a.Q = Q; a.Kp = K_prefix; a.Vp = V_prefix; a.Kc = K_cache; a.Vc = V_cache; a.len = len; a.q_len = q_len; a.O = O; a.weight = weight;
+  a.H = pl.H; a.Hk = pl.Hk; a.G = pl.G; a.T = pl.T; a.R = pl.R; a.cap = pl.cap; a.max_len = pl.max_len; a.each = pl.each; a.P = pl.P;
+  a.rows = pl.B * pl.H * pl.T;
+  a.scale2 = pl.scale * 1.44269504088896340736f;
+  int bits = 1;  // 2^bits is more than twice the keys of a row
+  while ((1LL << bits) <= 2LL * pl.P + 2LL * pl.max_len) bits++;
+  a.offset = c->dtype == TC_F16 ? 0.f : (float)bits;  // (half: its values times float32 sums are far from that range, and small halves lose bits)
+  char* w = static_cast<char*>(ws);
+  a.lse = weight ? reinterpret_cast<float*>(w) : nullptr;
+  w += align256((size_t)a.rows * 4);
+  a.ml = reinterpret_cast<f2*>(w);
+  w += align256(part_rows(pl) * 8);
+  a.part = reinterpret_cast<float*>(w);
+  const hipStream_t st = (hipStream_t)stream;
+  if (pl.dh == 64)
+    return c->dtype == TC_F32 ? attention_launch<float, 64>(pl, a, st) : c->dtype == TC_BF16 ? attention_launch<uint16_t, 64>(pl, a, st)
+                                                                                              : attention_launch<f16_t, 64>(pl, a, st);
+  return c->dtype == TC_F32 ? attention_launch<float, 128>(pl, a, st) : c->dtype == TC_BF16 ? attention_launch<uint16_t, 128>(pl, a, st)
+                                                                                            : attention_launch<f16_t, 128>(pl, a, st);
+}

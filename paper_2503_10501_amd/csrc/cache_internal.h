@@ -60,6 +60,7 @@ struct CachePlan {
 };
 int make_cache_plan(const tc_cache* c, CachePlan* plan);
 size_t evict_bytes(const CachePlan& pl);
+size_t attention_bytes(const CachePlan& pl);
 
 inline int check_cache_ws(const CachePlan& pl, const void* ws, size_t ws_bytes) {
   if (!ws) return TC_ERR_NULL;

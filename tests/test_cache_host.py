@@ -89,11 +89,12 @@ def _calls(tc, **change):
     lib, F = tc.load_library(), FAKE
     st = ctypes.byref(tc.tc_strides(1024, 64, 256))
     a = dict(c=None, r=ctypes.byref(tc.make_rope(64)), Q=F, qs=st, K=F, ks=st, V=F, vs=st, cos=F, sin=F, pos=F, len=F, q_len=F, Qo=F, Kc=F, Vc=F,
-             sp=F, w=F, Ko=2 * F, Vo=2 * F, po=2 * F, wo=2 * F, cap=50, lo=2 * F, ws=F, bytes=1 << 40)
+             sp=F, w=F, Kp=F, Vp=F, O=2 * F, Ko=2 * F, Vo=2 * F, po=2 * F, wo=2 * F, cap=50, lo=2 * F, ws=F, bytes=1 << 40)
     a.update(change)
     v = lambda *names: [a[n] for n in names]  # noqa: E731
     return {
         "append": lambda: lib.tc_cache_append(*v("c", "r", "Q", "qs", "K", "ks", "V", "vs", "cos", "sin", "pos", "len", "q_len", "Qo", "Kc", "Vc", "sp", "w"), None),
+        "attention": lambda: lib.tc_cache_attention(*v("c", "Q", "Kp", "Vp", "Kc", "Vc", "len", "q_len", "O", "w", "ws", "bytes"), None),
         "evict": lambda: lib.tc_cache_evict(*v("c", "len", "Kc", "Vc", "sp", "w", "Ko", "Vo", "po", "wo", "cap", "lo", "ws", "bytes"), None),
     }
 
@@ -121,6 +122,7 @@ def test_cache_entry_points_check_their_arguments():
     c = tc.make_cache(**CACHE)
     ok = ctypes.byref(c)
     needed = {"append": ("Q", "qs", "K", "ks", "V", "vs", "cos", "sin", "pos", "len", "Qo", "Kc", "Vc", "sp", "w"),
+              "attention": ("Q", "Kp", "Vp", "Kc", "Vc", "len", "O", "ws"),
               "evict": ("len", "Kc", "Vc", "sp", "w", "Ko", "Vo", "po", "wo", "lo", "ws")}
     for entry, names in needed.items():
         for name in names:
@@ -130,6 +132,8 @@ def test_cache_entry_points_check_their_arguments():
         assert _calls(tc, c=None)[entry]() == -1
         empty = ctypes.byref(tc.make_cache(**dict(CACHE, batch=0)))
         assert _calls(tc, c=empty, **{name: None for name in names})[entry]() == 0
+    assert _calls(tc, c=ok, w=FAKE + 4)["attention"]() == -6 and _calls(tc, c=ok, q_len=FAKE + 4)["attention"]() == -6
+    assert _calls(tc, c=ok, bytes=tc.tc_cache_workspace_bytes(c) - 1)["attention"]() == -5
     odd = ctypes.byref(tc.tc_strides(1024, 64, 4))
     for name in ("qs", "ks", "vs"):
         assert _calls(tc, c=ok, **{name: odd})["append"]() == -2
@@ -164,6 +168,57 @@ def test_oracle_appends_the_last_slots():
     assert w.tolist() == [[1, 1, 0, 0, 1]] * 2 and not K[:, [0, 1, 4]].any()
     orc.append(K, V, p, w, k, -k, [7, 9], 6)    # the second one falls behind the cache
     assert np.array_equal(K[:, 4], k[:, 0])
+
+
+def test_oracle_attention_by_a_softmax_and_closed_forms():
+    g = np.random.default_rng(4)
+    q, K, V, Kp, Vp = (g.normal(size=s) for s in ((4, 3, 8), (2, 10, 8), (2, 10, 8), (2, 5, 8), (2, 5, 8)))
+    O, W = orc.attention(q, K, V, 7, 3, Kp, Vp)
+    for h in range(4):
+        j = h // 2
+        keys, vals = np.concatenate([Kp[j], K[j, :7]]), np.concatenate([Vp[j], V[j, :7]])
+        s = q[h] @ keys.T / np.sqrt(8)
+        for t in range(3):
+            s[t, 5 + 7 - 3 + t + 1:] = -np.inf
+        p = np.exp(s) / np.exp(s).sum(1, keepdims=True)
+        assert np.allclose(O[:, h], p @ vals)
+    assert np.isclose(W[:, :7].sum() + _prefix_share(q, K, Kp), 12.0) and not W[:, 7:].any()
+    # equal keys: the mean of the values seen; no key at all: zero; padded rows: zero
+    O, W = orc.attention(q, np.ones_like(K), V, 2, 2)
+    assert np.allclose(O[0, 0], V[0, 0]) and np.allclose(O[1, 3], V[1, :2].mean(0)) and not O[2].any()
+    assert np.allclose(W[0, :2], [2 * 1.5, 2 * 0.5])
+    O, W = orc.attention(q, K, V, 0, 3)
+    assert not O.any() and not W.any()
+    O, W = orc.attention(q, K, V, 2, 3)        # the first of three tokens lies in front of the cache
+    assert not O[0].any() and np.allclose(O[1, 0], V[0, 0])
+
+
+def _prefix_share(q, K, Kp):
+    total = 0.0
+    for h in range(4):
+        for t in range(3):
+            s = np.exp(np.concatenate([Kp[h // 2], K[h // 2, :5 + t]]) @ q[h, t] / np.sqrt(8))
+            total += s[:5].sum() / s.sum()
+    return total
+
+
+@pytest.mark.parametrize("mistake", ["later", "prefix", "head", "scale", "weight"])
+def test_planted_mistakes_move_the_oracle(mistake):
+    """What the comparisons on the GPU rest on: each of these mistakes, planted here, is far outside their bounds."""
+    g = np.random.default_rng(5)
+    q, K, V, Kp, Vp = (g.normal(size=s) for s in ((4, 3, 64), (2, 40, 64), (2, 40, 64), (2, 20, 64), (2, 20, 64)))
+    O, W = orc.attention(q, K, V, 30, 3, Kp, Vp)
+    if mistake == "later":       # the rows see one slot too many
+        P, X = orc.attention(q, K, V, 31, 3, Kp, Vp)
+    elif mistake == "prefix":    # a prefix without its last key
+        P, X = orc.attention(q, K, V, 30, 3, Kp[:, :-1], Vp[:, :-1])
+    elif mistake == "head":      # heads dealt to key heads in turn
+        P, X = orc.attention(q[[0, 2, 1, 3]], K, V, 30, 3, Kp, Vp)
+    elif mistake == "scale":
+        P, X = orc.attention(q, K, V, 30, 3, Kp, Vp, scale=0.13)
+    else:                        # a row of a head that does not share the slot
+        P, X = O, orc.attention(q[[0, 0, 2, 3]], K, V, 30, 3, Kp, Vp)[1]
+    assert np.abs(O - P).max() > 0.02 or np.abs(W - X).max() > 0.02
 
 
 def test_oracle_evicts_by_protection_weight_and_slot():
