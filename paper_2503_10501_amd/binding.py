@@ -281,91 +281,88 @@ def tc_kv_cache_fraction(n_text, n_vis, n_kept, n_layers, n_layers_before):
     return float(load_library().tc_kv_cache_fraction(n_text, n_vis, n_kept, n_layers, n_layers_before))
 
 
-# ---- behind the compression: the tensors' shapes are checked, and work goes to the device that holds them
+# ---- behind the compression: the tensors' shapes are checked, and work goes to the device that holds them.  A decoding step makes these
+# calls for every layer: they keep to what a check costs (15 tensors: 5 us).
 
-def _shape(name, t, shape, dtype, device):
+_I32, _F32, _U8 = torch.int32, torch.float32, torch.uint8
+_STORAGE = {TC_F32: torch.float32, TC_BF16: torch.bfloat16, TC_F16: torch.float16}
+_CODES = {v: k for k, v in _STORAGE.items()}
+
+
+def _refuse(name, t, shape, dtype, dev):
     if t.dtype != dtype:
         raise ValueError("%s: expected %s, got %s" % (name, dtype, t.dtype))
     if tuple(t.shape) != tuple(shape):
         raise ValueError("%s: expected shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
-    if not t.is_cuda or t.device != device:
+    if t.get_device() != dev or dev < 0:
         raise ValueError("%s: tensors must be on one GPU" % name)
+    raise ValueError("%s: must be contiguous" % name)
 
 
-def _whole(name, t, shape, dtype, device):
+def _whole(name, t, shape, dtype, dev):
     """Address of a contiguous tensor (None for None)."""
     if t is None:
         return None
-    _shape(name, t, shape, dtype, device)
-    if not t.is_contiguous():
-        raise ValueError("%s: must be contiguous" % name)
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        _refuse(name, t, shape, dtype, dev)
     return t.data_ptr()
 
 
-def _rows(name, t, shape, dtype, device):
+def _rows(name, t, shape, dtype, dev):
     """Address and strides of a [batch, head, row, d_h] view with contiguous rows."""
-    _shape(name, t, shape, dtype, device)
-    if t.stride(3) != 1:
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        _refuse(name, t, shape, dtype, dev)
+    b, h, r, e = t.stride()
+    if e != 1:
         raise ValueError("%s: the elements of a row must be contiguous" % name)
-    return t.data_ptr(), ctypes.byref(tc_strides(t.stride(0), t.stride(1), t.stride(2)))
-
-
-class _on(object):
-    """The device of a call: its current stream, or the caller's."""
-
-    def __init__(self, device, stream):
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-        self.device, self.stream = device, stream
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return torch.cuda.current_stream(self.device).cuda_stream if self.stream is None else self.stream
-
-    def __exit__(self, *args):
-        if self.guard is not None:
-            self.guard.__exit__(*args)
+    return t.data_ptr(), ctypes.byref(tc_strides(b, h, r))
 
 
 def _device(name, t):
-    if not t.is_cuda:
+    dev = t.get_device()
+    if dev < 0:
         raise ValueError("%s: tensors must be on the GPU" % name)
-    return t.device
+    return dev
+
+
+def _call(entry, dev, stream, *args):
+    """The entry point on the device that holds the tensors: on its current stream, or the caller's."""
+    if stream is None:
+        stream = torch._C._cuda_getCurrentRawStream(dev)
+    if dev == torch._C._cuda_getDevice():
+        rc = entry(*args, stream)
+    else:
+        with torch.cuda.device(dev):
+            rc = entry(*args, stream)
+    if rc != 0:
+        _check(rc)
 
 
 def _rot(r):
     return r.rot_dim if r.rot_dim > 0 else r.head_dim
 
 
-def _dtype_of(name, t):
-    for code, dtype in ((TC_BF16, torch.bfloat16), (TC_F16, torch.float16), (TC_F32, torch.float32)):
-        if t.dtype == dtype:
-            return code
-    raise ValueError("%s: %s is no storage type" % (name, t.dtype))
-
-
 def tc_rope_tables(r, pos_ids, cos, sin, stream=None):
     """cos, sin: the shape of pos_ids and r/2 behind it."""
-    dev = _device("pos_ids", pos_ids)
-    shape = tuple(pos_ids.shape) + (_rot(r) // 2,)
-    pos = _whole("pos_ids", pos_ids, pos_ids.shape, torch.int32, dev)
-    c, s = _whole("cos", cos, shape, torch.float32, dev), _whole("sin", sin, shape, torch.float32, dev)
-    with _on(dev, stream) as st:
-        _check(load_library().tc_rope_tables(ctypes.byref(r), pos, pos_ids.numel(), c, s, st))
+    dev, shape = _device("pos_ids", pos_ids), pos_ids.shape
+    tables = (*shape, _rot(r) // 2)
+    _call(load_library().tc_rope_tables, dev, stream, r, _whole("pos_ids", pos_ids, shape, _I32, dev), pos_ids.numel(),
+          _whole("cos", cos, tables, _F32, dev), _whole("sin", sin, tables, _F32, dev))
 
 
 def tc_rope_apply(r, x, cos, sin, y=None, transposed=False, stream=None):
     """x, y: [batch, heads, rows, head_dim] views; without y the rows of x are turned in place."""
-    dev = _device("x", x)
-    y = x if y is None else y
-    if x.dim() != 4 or x.shape[3] != r.head_dim:
-        raise ValueError("x: expected [batch, heads, rows, %d], got %s" % (r.head_dim, tuple(x.shape)))
-    B, H, T, _ = x.shape
-    px, xs = _rows("x", x, x.shape, x.dtype, dev)
-    py, ys = _rows("y", y, x.shape, x.dtype, dev)
-    c, s = (_whole(n, t, (B, T, _rot(r) // 2), torch.float32, dev) for n, t in (("cos", cos), ("sin", sin)))
-    with _on(dev, stream) as st:
-        _check(load_library().tc_rope_apply(ctypes.byref(r), _dtype_of("x", x), B, H, T, px, xs, c, s, py, ys, int(transposed), st))
+    dev, sd, shape = _device("x", x), x.dtype, x.shape
+    if x.dim() != 4 or shape[3] != r.head_dim:
+        raise ValueError("x: expected [batch, heads, rows, %d], got %s" % (r.head_dim, tuple(shape)))
+    if sd not in _CODES:
+        raise ValueError("x: %s is no storage type" % sd)
+    B, H, T, _ = shape
+    px, xs = _rows("x", x, shape, sd, dev)
+    py, ys = (px, xs) if y is None else _rows("y", y, shape, sd, dev)
+    tables = (B, T, _rot(r) // 2)
+    _call(load_library().tc_rope_apply, dev, stream, r, _CODES[sd], B, H, T, px, xs, _whole("cos", cos, tables, _F32, dev),
+          _whole("sin", sin, tables, _F32, dev), py, ys, int(transposed))
 
 
 def tc_cache_workspace_bytes(c):
@@ -379,61 +376,50 @@ def new_cache_workspace(c, device="cuda"):
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _cached(c, K_cache, V_cache, lens, q_len, dev):
-    """Addresses of what every call on a cache takes: keys, values, lengths."""
-    shape = (c.batch, c.n_kv_heads, c.capacity, c.head_dim)
-    sd = storage_dtype(c)
-    return (_whole("K_cache", K_cache, shape, sd, dev), _whole("V_cache", V_cache, shape, sd, dev),
-            _whole("lens", lens, (c.batch,), torch.int32, dev), _whole("q_len", q_len, (c.batch,), torch.int32, dev))
-
-
 def tc_cache_append(c, r, Q, K, V, cos, sin, pos_ids, lens, Q_out, K_cache, V_cache, slot_pos, weight, q_len=None, stream=None):
     """Q [B, H, T, d], K, V [B, H_kv, T, d]: views; r, cos and sin None: nothing is turned."""
-    dev, sd = _device("Q", Q), storage_dtype(c)
-    B, T, d, slots = c.batch, c.n_query, c.head_dim, (c.batch, c.n_kv_heads, c.capacity)
-    q, qs = _rows("Q", Q, (B, c.n_heads, T, d), sd, dev)
-    k, ks = _rows("K", K, (B, c.n_kv_heads, T, d), sd, dev)
-    v, vs = _rows("V", V, (B, c.n_kv_heads, T, d), sd, dev)
-    co, si = (_whole(n, t, (B, T, _rot(r) // 2 if r is not None else 0), torch.float32, dev) for n, t in (("cos", cos), ("sin", sin)))
-    kc, vc, ln, ql = _cached(c, K_cache, V_cache, lens, q_len, dev)
-    pos, out = _whole("pos_ids", pos_ids, (B, T), torch.int32, dev), _whole("Q_out", Q_out, (B, c.n_heads, T, d), sd, dev)
-    sp, w = _whole("slot_pos", slot_pos, slots, torch.int32, dev), _whole("weight", weight, slots, torch.float32, dev)
-    with _on(dev, stream) as st:
-        _check(load_library().tc_cache_append(ctypes.byref(c), None if r is None else ctypes.byref(r), q, qs, k, ks, v, vs, co, si, pos, ln,
-                                              ql, out, kc, vc, sp, w, st))
+    dev, sd = _device("Q", Q), _STORAGE[c.dtype]
+    B, H, Hk, T, d, cap = c.batch, c.n_heads, c.n_kv_heads, c.n_query, c.head_dim, c.capacity
+    tables, slots, rows = (B, T, _rot(r) // 2 if r is not None else 0), (B, Hk, cap), (B, Hk, T, d)
+    q, qs = _rows("Q", Q, (B, H, T, d), sd, dev)
+    k, ks = _rows("K", K, rows, sd, dev)
+    v, vs = _rows("V", V, rows, sd, dev)
+    cache = (B, Hk, cap, d)
+    _call(load_library().tc_cache_append, dev, stream, c, r, q, qs, k, ks, v, vs, _whole("cos", cos, tables, _F32, dev),
+          _whole("sin", sin, tables, _F32, dev), _whole("pos_ids", pos_ids, (B, T), _I32, dev), _whole("lens", lens, (B,), _I32, dev),
+          _whole("q_len", q_len, (B,), _I32, dev), _whole("Q_out", Q_out, (B, H, T, d), sd, dev), _whole("K_cache", K_cache, cache, sd, dev),
+          _whole("V_cache", V_cache, cache, sd, dev), _whole("slot_pos", slot_pos, slots, _I32, dev),
+          _whole("weight", weight, slots, _F32, dev))
 
 
 def tc_cache_attention(c, Q, K_cache, V_cache, lens, O, ws, K_prefix=None, V_prefix=None, weight=None, q_len=None, stream=None):
-    dev, sd = _device("Q", Q), storage_dtype(c)
-    B, H, Hk, T, d = c.batch, c.n_heads, c.n_kv_heads, c.n_query, c.head_dim
-    q = _whole("Q", Q, (B, H, T, d), sd, dev)
-    prefix = (c.n_prefixes, Hk, c.prefix_len, d)
-    if c.prefix_len > 0 and (K_prefix is None or V_prefix is None):
+    dev, sd = _device("Q", Q), _STORAGE[c.dtype]
+    B, H, Hk, T, d, cap = c.batch, c.n_heads, c.n_kv_heads, c.n_query, c.head_dim, c.capacity
+    cache, prefix = (B, Hk, cap, d), (c.n_prefixes, Hk, c.prefix_len, d)
+    if prefix[2] > 0 and (K_prefix is None or V_prefix is None):
         raise ValueError("K_prefix, V_prefix: expected shape %s" % (prefix,))
-    kp, vp = _whole("K_prefix", K_prefix, prefix, sd, dev), _whole("V_prefix", V_prefix, prefix, sd, dev)
-    kc, vc, ln, ql = _cached(c, K_cache, V_cache, lens, q_len, dev)
-    o, w = _whole("O", O, (B, T, H * d), sd, dev), _whole("weight", weight, (B, Hk, c.capacity), torch.float32, dev)
-    work = _whole("ws", ws, ws.shape, torch.uint8, dev)
-    with _on(dev, stream) as st:
-        _check(load_library().tc_cache_attention(ctypes.byref(c), q, kp, vp, kc, vc, ln, ql, o, w, work, ws.numel(), st))
+    _call(load_library().tc_cache_attention, dev, stream, c, _whole("Q", Q, (B, H, T, d), sd, dev),
+          _whole("K_prefix", K_prefix, prefix, sd, dev), _whole("V_prefix", V_prefix, prefix, sd, dev),
+          _whole("K_cache", K_cache, cache, sd, dev), _whole("V_cache", V_cache, cache, sd, dev), _whole("lens", lens, (B,), _I32, dev),
+          _whole("q_len", q_len, (B,), _I32, dev), _whole("O", O, (B, T, H * d), sd, dev), _whole("weight", weight, (B, Hk, cap), _F32, dev),
+          _whole("ws", ws, (ws.numel(),), _U8, dev), ws.numel())
 
 
 def tc_cache_evict(c, lens, K_cache, V_cache, slot_pos, weight, len_out, ws, K_out=None, V_out=None, pos_out=None, weight_out=None,
                    stream=None):
     """Without K_out, V_out, pos_out, weight_out [B, H_kv, out_capacity(, d)]: in place."""
-    dev, sd, slots = _device("K_cache", K_cache), storage_dtype(c), (c.batch, c.n_kv_heads, c.capacity)
-    kc, vc, ln, _ = _cached(c, K_cache, V_cache, lens, None, dev)
-    sp, w = _whole("slot_pos", slot_pos, slots, torch.int32, dev), _whole("weight", weight, slots, torch.float32, dev)
-    given = [t is not None for t in (K_out, V_out, pos_out, weight_out)]
-    if any(given) != all(given):
-        raise ValueError("K_out, V_out, pos_out and weight_out are given together")
-    cap = int(K_out.shape[2]) if all(given) and K_out.dim() == 4 else c.capacity
+    dev, sd = _device("K_cache", K_cache), _STORAGE[c.dtype]
+    B, Hk, d, cap = c.batch, c.n_kv_heads, c.head_dim, c.capacity
+    cache, slots = (B, Hk, cap, d), (B, Hk, cap)
+    kc, vc = _whole("K_cache", K_cache, cache, sd, dev), _whole("V_cache", V_cache, cache, sd, dev)
+    sp, w = _whole("slot_pos", slot_pos, slots, _I32, dev), _whole("weight", weight, slots, _F32, dev)
     ko, vo, po, wo = kc, vc, sp, w
-    if all(given):
-        out = (c.batch, c.n_kv_heads, cap)
-        ko, vo = _whole("K_out", K_out, out + (c.head_dim,), sd, dev), _whole("V_out", V_out, out + (c.head_dim,), sd, dev)
-        po, wo = _whole("pos_out", pos_out, out, torch.int32, dev), _whole("weight_out", weight_out, out, torch.float32, dev)
-    lo = _whole("len_out", len_out, (c.batch,), torch.int32, dev)
-    work = _whole("ws", ws, ws.shape, torch.uint8, dev)
-    with _on(dev, stream) as st:
-        _check(load_library().tc_cache_evict(ctypes.byref(c), ln, kc, vc, sp, w, ko, vo, po, wo, cap, lo, work, ws.numel(), st))
+    if K_out is not None or V_out is not None or pos_out is not None or weight_out is not None:
+        if K_out is None or V_out is None or pos_out is None or weight_out is None:
+            raise ValueError("K_out, V_out, pos_out and weight_out are given together")
+        cap = K_out.shape[2] if K_out.dim() == 4 else cap
+        cache, slots = (B, Hk, cap, d), (B, Hk, cap)
+        ko, vo = _whole("K_out", K_out, cache, sd, dev), _whole("V_out", V_out, cache, sd, dev)
+        po, wo = _whole("pos_out", pos_out, slots, _I32, dev), _whole("weight_out", weight_out, slots, _F32, dev)
+    _call(load_library().tc_cache_evict, dev, stream, c, _whole("lens", lens, (B,), _I32, dev), kc, vc, sp, w, ko, vo, po, wo, cap,
+          _whole("len_out", len_out, (B,), _I32, dev), _whole("ws", ws, (ws.numel(),), _U8, dev), ws.numel())

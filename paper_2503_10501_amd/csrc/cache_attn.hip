@@ -108,10 +108,23 @@ struct AttnArgs {
   float* lse;   // [row]: base-2 logarithm of the sum of all probabilities' numerators; +inf: the row gives nothing to anyone
   int H, Hk, G, T, R, cap, max_len, each, P;
   int rows;     // all rows: B H T
-  int splits;   // parts of the keys
+  int parts;    // parts of the keys of a row
   float scale2; // scale log2(e)
   float offset; // probabilities are formed as 2^(s - m - offset), so that sums of them times values stay within float32
 };
+
+// A share of a call: the rows of a group against the keys of a prefix, of the group's cache, or both.  A group is what has one
+// key/value head in common: a sequence's R rows, or, `packed`, the rows of all sequences of an image, which then read its prefix once.
+struct Job {
+  int groups, rows, tiles, splits, part0;  // part0: the first of the `splits` parts that this share writes
+  bool packed, prefix, cache;
+};
+
+// Row r of a group: its place among all rows.
+__device__ inline int row_of(const AttnArgs& a, const Job& j, int group, int r) {
+  if (!j.packed) return group * a.R + r;
+  return ((group / a.Hk * a.each + r / a.R) * a.Hk + group % a.Hk) * a.R + r % a.R;
+}
 
 // Row r of a sequence: what it sees of the cache.  Rows behind the last token see what that one sees; nothing of them is kept.
 __device__ inline int seen(const AttnArgs& a, int r, int n, int m) {
@@ -160,7 +173,7 @@ struct FewShape {
 };
 
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void few_kernel(AttnArgs a, int tiles) {
+__global__ __launch_bounds__(256) void few_kernel(AttnArgs a, Job first, Job second) {
   typedef FewShape<T, DH> S;
   typedef Mma<T> M;
   typedef typename M::frag frag;
@@ -168,14 +181,22 @@ __global__ __launch_bounds__(256) void few_kernel(AttnArgs a, int tiles) {
   extern __shared__ __attribute__((aligned(16))) unsigned char cache_smem[];
   __shared__ float wave_m[4][16], wave_l[4][16], row_sum[16];  // row_sum: infinite for a row whose output is zero
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
-  const unsigned item = blockIdx.x;
-  const int split = item % a.splits, tile = item / a.splits % tiles;
-  const unsigned bh = item / a.splits / tiles;
-  const int b = bh / a.Hk, hk = bh % a.Hk;
-  const int n = clamp_len(a.len[b], a.max_len), m = a.q_len ? clamp_len(a.q_len[b], a.T) : a.T;
-  const int r = tile * 16 + i, row = bh * a.R + r;  // this lane's row of queries
-  const bool live = r < a.R && r % a.T < m;
-  const int end = m > 0 ? seen(a, min(r, a.R - 1), n, m) : 0;
+  const unsigned in_first = (unsigned)first.groups * first.tiles * first.splits;
+  const bool other = blockIdx.x >= in_first;
+  const Job job = other ? second : first;
+  const unsigned item = blockIdx.x - (other ? in_first : 0);
+  const int split = item % job.splits, tile = item / job.splits % job.tiles;
+  const int group = item / job.splits / job.tiles, hk = group % a.Hk, b = group / a.Hk;  // (packed: b is the image)
+  const int r = tile * 16 + i, row = row_of(a, job, group, min(r, job.rows - 1));  // this lane's row of queries
+  const bool mine = r < job.rows;
+  int n = 0, m = 1, end = 0;
+  bool live = mine;
+  if (job.cache) {
+    n = clamp_len(a.len[b], a.max_len);
+    m = a.q_len ? clamp_len(a.q_len[b], a.T) : a.T;
+    live = mine && r % a.T < m;
+    end = m > 0 ? seen(a, min(r, a.R - 1), n, m) : 0;
+  }
   int most = end, least = end;
 #pragma unroll
   for (int o = 1; o < 16; o <<= 1) {
@@ -185,10 +206,10 @@ __global__ __launch_bounds__(256) void few_kernel(AttnArgs a, int tiles) {
   most = __builtin_amdgcn_readfirstlane(most);
   least = __builtin_amdgcn_readfirstlane(least);
   // tiles of the prefix, then of the cache; this workgroup's share of them, dealt to its wavefronts in turn
-  const int np = m > 0 ? (a.P + FK - 1) / FK : 0, all = np + (most + FK - 1) / FK;
-  const int t0 = (int)((long long)all * split / a.splits), t1 = (int)((long long)all * (split + 1) / a.splits);
+  const int np = job.prefix && m > 0 ? (a.P + FK - 1) / FK : 0, all = np + (most + FK - 1) / FK;
+  const int t0 = (int)((long long)all * split / job.splits), t1 = (int)((long long)all * (split + 1) / job.splits);
 
-  const size_t head = (size_t)bh * a.cap, phead = a.P > 0 ? ((size_t)(b / a.each) * a.Hk + hk) * a.P : 0;
+  const size_t head = (size_t)group * a.cap, phead = job.prefix ? ((size_t)(job.packed ? b : b / a.each) * a.Hk + hk) * a.P : 0;
   unsigned char* Ks = cache_smem + wave * S::WAVE;
   unsigned char* Vs = Ks + FK * S::KLD;
   u4 kr[NV], vr[NV];
@@ -209,7 +230,7 @@ __global__ __launch_bounds__(256) void few_kernel(AttnArgs a, int tiles) {
 
   frag q[DH / 32];
   {
-    const u4* Qr = reinterpret_cast<const u4*>(static_cast<const T*>(a.Q) + (size_t)(bh * a.R + min(r, a.R - 1)) * DH);
+    const u4* Qr = reinterpret_cast<const u4*>(static_cast<const T*>(a.Q) + (size_t)row * DH);
 #pragma unroll
     for (int s = 0; s < DH / 32; s++) q[s] = frag_of<T>(Qr, 4 * s + g);
   }
@@ -344,22 +365,22 @@ __global__ __launch_bounds__(256) void few_kernel(AttnArgs a, int tiles) {
   float* part = reinterpret_cast<float*>(cache_smem + wave * S::WAVE);
 #pragma unroll
   for (int d = 0; d < DT; d++) *reinterpret_cast<f4*>(part + i * (DH + 4) + 16 * d + 4 * g) = o[d] * f;
-  if (threadIdx.x < 16 && r < a.R) {  // (wavefront 0, lane i: row i)
-    if (a.splits > 1) a.ml[(size_t)split * a.rows + row] = f2{top == -INFINITY ? top : top + a.offset, total};
+  if (threadIdx.x < 16 && mine) {  // (wavefront 0, lane i: row i)
+    if (a.parts > 1) a.ml[(size_t)(job.part0 + split) * a.rows + row] = f2{top == -INFINITY ? top : top + a.offset, total};
     else if (a.lse) a.lse[row] = live ? ref + a.offset + log2f(total) : INFINITY;
     row_sum[i] = live && a.P + end > 0 ? total : INFINITY;
   }
   __syncthreads();
-  if (a.splits > 1 && t0 >= t1) return;
+  if (a.parts > 1 && t0 >= t1) return;
   for (int at = threadIdx.x; at < 16 * DH / 4; at += 256) {
     const int rr = at / (DH / 4), c = at % (DH / 4);
-    if (tile * 16 + rr >= a.R) continue;
+    if (tile * 16 + rr >= job.rows) continue;
     f4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < 4; w++) v += *reinterpret_cast<const f4*>(cache_smem + w * S::WAVE + (rr * (DH + 4) + 4 * c) * 4);
-    const int to = bh * a.R + tile * 16 + rr;
-    if (a.splits > 1) {
-      *reinterpret_cast<f4*>(a.part + ((size_t)split * a.rows + to) * DH + 4 * c) = v;
+    const int to = row_of(a, job, group, tile * 16 + rr);
+    if (a.parts > 1) {
+      *reinterpret_cast<f4*>(a.part + ((size_t)(job.part0 + split) * a.rows + to) * DH + 4 * c) = v;
     } else {
       v = row_sum[rr] < INFINITY || row_sum[rr] != row_sum[rr] ? v / row_sum[rr] : f4{0.f, 0.f, 0.f, 0.f};
       T* out = static_cast<T*>(a.O) + out_row(a, to, DH) + 4 * c;
@@ -378,12 +399,12 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
   const int n = clamp_len(a.len[b], a.max_len), m = a.q_len ? clamp_len(a.q_len[b], a.T) : a.T;
   const bool live = t < m && a.P + clamp_len(n - m + t + 1, n) > 0;
   float top = -INFINITY;
-  for (int s = 0; s < a.splits; s++) top = fmaxf(top, a.ml[(size_t)s * a.rows + row][0]);
+  for (int s = 0; s < a.parts; s++) top = fmaxf(top, a.ml[(size_t)s * a.rows + row][0]);
   const float ref = top == -INFINITY ? 0.f : top;
   float total = 0.f, v[DH / 64];
 #pragma unroll
   for (int e = 0; e < DH / 64; e++) v[e] = 0.f;
-  for (int s = 0; s < a.splits; s++) {
+  for (int s = 0; s < a.parts; s++) {
     const f2 x = a.ml[(size_t)s * a.rows + row];
     if (x[0] == -INFINITY && x[1] == 0.f) continue;  // saw nothing: its part is not written
     const float f = exp2_fast(x[0] - ref);
@@ -434,19 +455,44 @@ __global__ __launch_bounds__(256) void gather_kernel(AttnArgs a, int chunks) {
   }
 }
 
-// Parts of the keys: enough workgroups for the chip, and no more than there are tiles for the wavefronts.
-static int few_splits(const CachePlan& pl) {
-  const long long items = (long long)pl.B * pl.Hk * ((pl.R + 15) / 16);
-  const int tiles = (pl.P + FK - 1) / FK + (pl.max_len + FK - 1) / FK;
-  long long s = items > 0 ? (1024 + items - 1) / items : 1;
+// How a call is cut.  The prefix of an image's sequences is read once for all of them where the rows of one sequence do not fill a
+// tile by themselves; else a sequence's rows go over its prefix and its cache in one sweep.
+constexpr int FEW_WG = 1024, FEW_ROWS = 16;
+static Job make_job(int groups, int rows, int keys, bool packed, bool prefix, bool cache) {
+  Job j = {groups, rows, (rows + FEW_ROWS - 1) / FEW_ROWS, 1, 0, packed, prefix, cache};
+  // parts of the keys: enough workgroups for the chip, and a tile for each wavefront
+  const long long items = (long long)groups * j.tiles, tiles = (keys + FK - 1) / FK + (prefix && cache ? 1 : 0);
+  long long s = (FEW_WG + items - 1) / items;
   if (s > (tiles + 3) / 4) s = (tiles + 3) / 4;
-  return s < 1 ? 1 : (int)s;
+  j.splits = s < 1 ? 1 : (int)s;
+  return j;
+}
+struct Cut {
+  int jobs;
+  Job job[2];
+  int parts;
+};
+static Cut make_cut(const CachePlan& pl, int max_len) {
+  Cut c = {};
+  if (pl.images > 0 && pl.each > 1 && pl.R < 128) {
+    c.jobs = 2;
+    c.job[0] = make_job(pl.images * pl.Hk, pl.each * pl.R, pl.P, true, true, false);
+    c.job[1] = make_job(pl.B * pl.Hk, pl.R, max_len, false, false, true);
+    c.job[1].part0 = c.job[0].splits;
+    c.parts = c.job[0].splits + c.job[1].splits;
+  } else {
+    c.jobs = 1;
+    c.job[0] = make_job(pl.B * pl.Hk, pl.R, pl.P + max_len, false, pl.P > 0, true);
+    c.parts = c.job[0].splits;
+  }
+  return c;
 }
 
-// Rows of parts: at most 1024 + items workgroups of 16 rows where keys are split, which they are below 1024 items.
+// Rows of parts (none where a row has a single one).
 static size_t part_rows(const CachePlan& pl) {
-  const long long items = (long long)pl.B * pl.Hk * ((pl.R + 15) / 16);
-  return (size_t)(1024 + (items < 1024 ? items : 1024)) * 16;
+  if (pl.B == 0) return 0;
+  const Cut c = make_cut(pl, pl.cap);  // (longer caches are cut into no fewer parts)
+  return c.parts > 1 ? (size_t)pl.B * pl.H * pl.T * c.parts : 0;
 }
 size_t attention_bytes(const CachePlan& pl) {
   return align256((size_t)pl.B * pl.H * pl.T * 4) + align256(part_rows(pl) * 8) + part_rows(pl) * pl.dh * 4;
@@ -455,15 +501,16 @@ size_t attention_bytes(const CachePlan& pl) {
 template <typename T, int DH>
 static int attention_launch(const CachePlan& pl, AttnArgs a, hipStream_t st) {
   typedef FewShape<T, DH> S;
-  const int tiles = (pl.R + 15) / 16;
-  a.splits = few_splits(pl);
-  const long long grid = (long long)pl.B * pl.Hk * tiles * a.splits, chunks = (pl.max_len + 63) / 64;
+  const Cut cut = make_cut(pl, pl.max_len);
+  a.parts = cut.parts;
+  long long grid = 0, chunks = (pl.max_len + 63) / 64;
+  for (int k = 0; k < cut.jobs; k++) grid += (long long)cut.job[k].groups * cut.job[k].tiles * cut.job[k].splits;
   if (grid > 0x7fffffffLL || (a.weight && chunks * pl.B * pl.Hk > 0x7fffffffLL)) return TC_ERR_SHAPE;
   if (S::LDS + 1024 > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(few_kernel<T, DH>),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS) != hipSuccess)
     return TC_ERR_HIP;
-  few_kernel<T, DH><<<(unsigned)grid, 256, S::LDS, st>>>(a, tiles);
-  if (a.splits > 1) join_kernel<T, DH><<<(a.rows + 3) / 4, 256, 0, st>>>(a);
+  few_kernel<T, DH><<<(unsigned)grid, 256, S::LDS, st>>>(a, cut.job[0], cut.job[cut.jobs - 1]);
+  if (a.parts > 1) join_kernel<T, DH><<<(a.rows + 3) / 4, 256, 0, st>>>(a);
   if (a.weight) gather_kernel<T, DH><<<(unsigned)(chunks * pl.B * pl.Hk), 256, 0, st>>>(a, (int)chunks);
   return check_launch();
 }
