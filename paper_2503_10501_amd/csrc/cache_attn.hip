@@ -19,6 +19,7 @@ typedef __attribute__((ext_vector_type(2))) unsigned int u2;
 typedef __attribute__((ext_vector_type(2))) float f2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf2;
 typedef __attribute__((ext_vector_type(2))) _Float16 h2;
+typedef __attribute__((ext_vector_type(16))) float f16v;
 
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }  // (results below the smallest normal number: 0)
 
@@ -29,6 +30,7 @@ template <> struct Mma<uint16_t> {
   typedef union { u4 u; uint32_t w[4]; bfrag v; short4v h[2]; } frag;
   static constexpr bool WIDE = true;  // exponents of float32: sums of unscaled probabilities times values could pass its range
   __device__ static inline f4 mul(const frag& a, const frag& b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0); }
+  static __device__ inline f16v mul32(const frag& a, const frag& b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0); }
   // two floats as packed 16-bit heads, and what this rounding leaves
   __device__ static inline uint32_t head(float x, float y) {
     union { bf2 v; uint32_t w; } h;
@@ -44,6 +46,7 @@ template <> struct Mma<f16_t> {
   typedef union { u4 u; uint32_t w[4]; hfrag v; short4v h[2]; } frag;
   static constexpr bool WIDE = false;
   __device__ static inline f4 mul(const frag& a, const frag& b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, b.v, c, 0, 0, 0); }
+  static __device__ inline f16v mul32(const frag& a, const frag& b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a.v, b.v, c, 0, 0, 0); }
   __device__ static inline uint32_t head(float x, float y) {
     union { h2 v; uint32_t w; } h;
     h.v = __builtin_convertvector(f2{x, y}, h2);
@@ -106,6 +109,8 @@ struct AttnArgs {
   f2* ml;       // [part][row]: running maximum (base 2, with the offset below) and sum
   float* part;  // [part][row][d_h]
   float* lse;   // [row]: base-2 logarithm of the sum of all probabilities' numerators; +inf: the row gives nothing to anyone
+  float* score; // [row][score_ld]: base-2 scores of the cache's keys, where rows are few
+  int score_ld;
   int H, Hk, G, T, R, cap, max_len, each, P;
   int rows;     // all rows: B H T
   int parts;    // parts of the keys of a row
@@ -117,7 +122,7 @@ struct AttnArgs {
 // key/value head in common: a sequence's R rows, or, `packed`, the rows of all sequences of an image, which then read its prefix once.
 struct Job {
   int groups, rows, tiles, splits, part0;  // part0: the first of the `splits` parts that this share writes
-  bool packed, prefix, cache;
+  bool packed, prefix, cache, many;        // many: by many_kernel
 };
 
 // Row r of a group: its place among all rows.
@@ -143,6 +148,12 @@ __device__ inline bool not_finite(T v) {
   if constexpr (sizeof(T) == 4) return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u;
   else if constexpr (Mma<T>::WIDE) return (v & 0x7f80u) == 0x7f80u;
   else return (__builtin_bit_cast(uint16_t, v) & 0x7c00u) == 0x7c00u;
+}
+// two packed values, those that are not finite as zero
+template <typename T>
+__device__ inline uint32_t finite_only(uint32_t w) {
+  return (not_finite<T>(__builtin_bit_cast(T, (uint16_t)w)) ? 0 : w & 0xffffu) |
+         (not_finite<T>(__builtin_bit_cast(T, (uint16_t)(w >> 16))) ? 0 : w & 0xffff0000u);
 }
 template <typename T>
 __device__ inline bool any_not_finite(const u4& w) {
@@ -275,6 +286,10 @@ __global__ __launch_bounds__(256) void few_kernel(AttnArgs a, Job first, Job sec
         s[u][e] = !masked || key < (pre ? last : end) ? s[u][e] * a.scale2 : -INFINITY;
         top = fmaxf(top, s[u][e]);
       }
+    if (a.score && !pre && mine) {
+#pragma unroll
+      for (int u = 0; u < 2; u++) *reinterpret_cast<f4*>(a.score + (size_t)row * a.score_ld + k0 + 16 * u + 4 * g) = s[u];
+    }
     top = fmaxf(mx, col_max(top));
     const float ref = top == -INFINITY ? 0.f : top + a.offset;
     if (__ballot(top > mx)) {
@@ -323,11 +338,7 @@ __global__ __launch_bounds__(256) void few_kernel(AttnArgs a, Job first, Job sec
           for (int j = 0; j < 8; j++) v.f[j] = not_finite(v.f[j]) ? 0.f : v.f[j];
         } else {
 #pragma unroll
-          for (int j = 0; j < 4; j++) {
-            const uint32_t w = v.w[j];
-            v.w[j] = (not_finite<T>(__builtin_bit_cast(T, (uint16_t)w)) ? 0 : w & 0xffffu) |
-                     (not_finite<T>(__builtin_bit_cast(T, (uint16_t)(w >> 16))) ? 0 : w & 0xffff0000u);
-          }
+          for (int j = 0; j < 4; j++) v.w[j] = finite_only<T>(v.w[j]);
         }
       }
       o[d] = M::mul(v, ph, o[d]);
@@ -390,32 +401,358 @@ __global__ __launch_bounds__(256) void few_kernel(AttnArgs a, Job first, Job sec
   }
 }
 
-// The parts of a row joined: one wavefront per row.
+// ---- many rows, 16-bit storage: one workgroup has 128 rows, a wavefront 32 of them, all go over the same tiles of 64 keys ----
+//
+// Products of 32 x 32 tiles: a lane has row lane % 32, and of each 32 keys those with (key / 4) % 2 = lane / 32, which are the ones that its
+// operand of the second product wants.  A tile is in one of two stages of LDS while the next one is written into the other and the one
+// after that comes to registers: one barrier a tile.
+constexpr int MK = 64, MROWS = 128;
+template <int DH>
+struct ManyShape {
+  static constexpr int VEC = DH / 8, NV = MK * VEC / 256;         // 16-byte vectors of a row, of a thread
+  static constexpr int KLD = DH * 2 + 16, VLD = DH * 2 + 64;      // rows in LDS: 16 lanes of a read meet other banks
+  static constexpr int STAGE = MK * (KLD + VLD), LDS = 2 * STAGE;
+  static_assert(4 * 32 * KLD <= LDS, "the output takes the place of the tiles");
+};
+// The running maximum is raised when a row's passes it by more than 2^8: up to there the probabilities are larger than 1, which neither
+// the sums in float32 nor the heads mind, and the partial output need not be scaled.
+constexpr float LAZY = 8.f;
+
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
-  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (row >= a.rows) return;
+struct ManyWave {
+  typedef Mma<T> M;
+  typedef typename M::frag frag;
+  typedef ManyShape<DH> S;
+  frag q[DH / 16];
+  f16v o[DH / 32];
+  float mx, sum;
+
+  // One tile.  MASKED: some row of the wavefront does not see some key; keys below `lim` are seen by this lane's row.
+  template <bool MASKED>
+  __device__ __forceinline__ void step(const unsigned char* Ks, const unsigned char* Vs, int k0, int lim, bool odd, float scale2, float offset,
+                                       int lane) {
+    const int half = lane >> 5, i = lane & 31;
+    f16v s[2];
+#pragma unroll
+    for (int e = 0; e < 16; e++) s[0][e] = s[1][e] = 0.f;
+    const unsigned char* kr = Ks + i * S::KLD + 16 * half;
+#pragma unroll
+    for (int c = 0; c < DH / 16; c++)
+#pragma unroll
+      for (int u = 0; u < 2; u++) {
+        frag k;
+        k.u = *reinterpret_cast<const u4*>(kr + u * 32 * S::KLD + 32 * c);
+        s[u] = M::mul32(k, q[c], s[u]);
+      }
+    if (MASKED) {
+#pragma unroll
+      for (int u = 0; u < 2; u++)
+#pragma unroll
+        for (int e = 0; e < 16; e++)
+          if (k0 + 32 * u + 8 * (e >> 2) + 4 * half + (e & 3) >= lim) s[u][e] = -INFINITY;
+    }
+    float top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < 2; u++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) top = fmaxf(top, s[u][e]);
+    const u2 w = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+    top = fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1])) * scale2;
+    if (__ballot(top > mx + LAZY)) {
+      const float now = fmaxf(mx, top), f = now == -INFINITY ? 1.f : exp2_fast(mx - now);
+      mx = now;
+      sum *= f;
+#pragma unroll
+      for (int d = 0; d < DH / 32; d++) o[d] *= f;
+    }
+    const float ref = mx == -INFINITY ? 0.f : mx + offset;
+#pragma unroll
+    for (int u = 0; u < 2; u++) {
+      float p[16];
+#pragma unroll
+      for (int e = 0; e < 16; e++) {
+        p[e] = exp2_fast(fmaf(s[u][e], scale2, -ref));
+        sum += p[e];
+      }
+#pragma unroll
+      for (int v = 0; v < 2; v++) {
+        // probabilities enter as they round to 16 bits: an error of the size of the output's own rounding, half of the products of
+        // the exact form
+        frag ph;
+#pragma unroll
+        for (int j = 0; j < 4; j++) ph.w[j] = M::head(p[8 * v + 2 * j], p[8 * v + 2 * j + 1]);
+#pragma unroll
+        for (int d = 0; d < DH / 32; d++) {
+          frag x;
+#pragma unroll
+          for (int j = 0; j < 2; j++) {
+            const unsigned char* at = Vs + (32 * u + 16 * v + 8 * j + 4 * half + (i & 15) / 4) * S::VLD + (32 * d + (i & 16) + 4 * (i & 3)) * 2;
+            x.h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)const_cast<unsigned char*>(at));
+          }
+          if (MASKED && odd) {
+#pragma unroll
+            for (int j = 0; j < 4; j++) x.w[j] = finite_only<T>(x.w[j]);
+          }
+          o[d] = M::mul32(x, ph, o[d]);
+        }
+      }
+    }
+    if (MASKED && odd) {  // values that are not finite reach the rows that see them, and no other
+      for (int k = 0; k < MK; k++) {
+        if (k0 + k >= lim) continue;
+#pragma unroll
+        for (int d = 0; d < DH / 32; d++)
+#pragma unroll
+          for (int e = 0; e < 16; e++) {
+            const T v = *reinterpret_cast<const T*>(Vs + k * S::VLD + (32 * d + 8 * (e >> 2) + 4 * half + (e & 3)) * 2);
+            if (not_finite(v)) o[d][e] += Vec16<T>::one(v);
+          }
+      }
+    }
+  }
+};
+
+template <typename T, int DH>
+__global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
+  typedef ManyShape<DH> S;
+  typedef ManyWave<T, DH> Wave;
+  extern __shared__ __attribute__((aligned(16))) unsigned char cache_smem[];
+  __shared__ int ends[2][4], flag[3];
+  int group, item;
+  if (!group_on_xcd(blockIdx.x, job.tiles * job.splits, job.groups, &group, &item)) return;
+  const int split = item % job.splits, tile = job.tiles - 1 - item / job.splits;  // (the rows that see the most first)
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, i = lane & 31;
+  const int hk = group % a.Hk, b = group / a.Hk;  // (packed: b is the image)
+  const int r = tile * MROWS + wave * 32 + i, row = row_of(a, job, group, min(r, job.rows - 1));
+  const bool mine = r < job.rows, idle = tile * MROWS + wave * 32 >= job.rows;
+  int m = 1, end = 0;
+  bool live = mine;
+  if (job.cache) {
+    const int n = clamp_len(a.len[b], a.max_len);
+    m = a.q_len ? clamp_len(a.q_len[b], a.T) : a.T;
+    live = mine && r % a.T < m;
+    end = m > 0 ? seen(a, min(r, a.R - 1), n, m) : 0;
+  }
+  int most = end, least = end;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    most = max(most, __shfl_xor(most, o, 64));
+    least = min(least, __shfl_xor(least, o, 64));
+  }
+  const int wave_most = __builtin_amdgcn_readfirstlane(most), wave_least = __builtin_amdgcn_readfirstlane(least);
+  if (lane == 0) {
+    ends[0][wave] = most;
+    ends[1][wave] = least;
+  }
+  if (tid < 3) flag[tid] = 0;
+  __syncthreads();
+  most = __builtin_amdgcn_readfirstlane(max(max(ends[0][0], ends[0][1]), max(ends[0][2], ends[0][3])));
+  least = __builtin_amdgcn_readfirstlane(min(min(ends[1][0], ends[1][1]), min(ends[1][2], ends[1][3])));
+  const int np = job.prefix && m > 0 ? (a.P + MK - 1) / MK : 0, all = np + (most + MK - 1) / MK;
+  const int t0 = (int)((long long)all * split / job.splits), t1 = (int)((long long)all * (split + 1) / job.splits);
+
+  const size_t head = (size_t)group * a.cap, phead = job.prefix ? ((size_t)(job.packed ? b : b / a.each) * a.Hk + hk) * a.P : 0;
+  u4 kr[S::NV], vr[S::NV];
+  // rows behind the last key are read as the last one, and their values as zero
+  auto fetch = [&](int t) {
+    const bool pre = t < np;
+    const int k0 = (pre ? t : t - np) * MK, last = (pre ? a.P : most) - 1;
+    const u4* K = reinterpret_cast<const u4*>(static_cast<const T*>(pre ? a.Kp : a.Kc) + (pre ? phead : head) * DH);
+    const u4* V = reinterpret_cast<const u4*>(static_cast<const T*>(pre ? a.Vp : a.Vc) + (pre ? phead : head) * DH);
+#pragma unroll
+    for (int j = 0; j < S::NV; j++) {
+      const int at = tid + 256 * j, key = k0 + at / S::VEC;
+      kr[j] = K[(size_t)min(key, last) * S::VEC + at % S::VEC];
+      const u4 v = V[(size_t)min(key, last) * S::VEC + at % S::VEC];
+      vr[j] = key <= last ? v : u4{0, 0, 0, 0};
+    }
+  };
+  auto store = [&](int t) {
+    unsigned char* Ks = cache_smem + (t & 1) * S::STAGE;
+    unsigned char* Vs = Ks + MK * S::KLD;
+    const bool pre = t < np;
+    if ((pre ? t : t - np) * MK + MK > (pre ? a.P : least)) {  // rows differ in what they see: is every value finite?
+      bool odd = false;
+#pragma unroll
+      for (int j = 0; j < S::NV; j++) odd |= any_not_finite<T>(vr[j]);
+      if (odd) flag[t % 3] = 1;
+    }
+#pragma unroll
+    for (int j = 0; j < S::NV; j++) {
+      const int at = tid + 256 * j, key = at / S::VEC, c = at % S::VEC;
+      *reinterpret_cast<u4*>(Ks + key * S::KLD + c * 16) = kr[j];
+      *reinterpret_cast<u4*>(Vs + key * S::VLD + c * 16) = vr[j];
+    }
+  };
+
+  Wave w;
+  {
+    const u4* Qr = reinterpret_cast<const u4*>(static_cast<const T*>(a.Q) + (size_t)row * DH);
+#pragma unroll
+    for (int c = 0; c < DH / 16; c++) w.q[c].u = Qr[2 * c + half];
+  }
+#pragma unroll
+  for (int d = 0; d < DH / 32; d++)
+#pragma unroll
+    for (int e = 0; e < 16; e++) w.o[d][e] = 0.f;
+  w.mx = -INFINITY;
+  w.sum = 0.f;
+  if (t0 < t1) {
+    fetch(t0);
+    store(t0);
+    if (t0 + 1 < t1) fetch(t0 + 1);
+    __syncthreads();
+  }
+  for (int t = t0; t < t1; t++) {
+    const bool pre = t < np;
+    const int k0 = (pre ? t : t - np) * MK, lim = pre ? a.P : end;
+    const unsigned char* Ks = cache_smem + (t & 1) * S::STAGE;
+    if (!idle && (pre || k0 < wave_most)) {
+      if (k0 + MK > (pre ? a.P : wave_least))
+        w.template step<true>(Ks, Ks + MK * S::KLD, k0, lim, flag[t % 3] != 0, a.scale2, a.offset, lane);
+      else
+        w.template step<false>(Ks, Ks + MK * S::KLD, k0, lim, false, a.scale2, a.offset, lane);
+    }
+    if (tid == 0) flag[(t + 2) % 3] = 0;  // (last looked at before the last barrier, set again behind the next one)
+    if (t + 1 < t1) store(t + 1);         // the other stage was last read before the last barrier
+    __syncthreads();
+    if (t + 2 < t1) fetch(t + 2);
+  }
+  const u2 x = __builtin_amdgcn_permlane32_swap(__float_as_uint(w.sum), __float_as_uint(w.sum), false, false);
+  const float total = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+  if (a.parts > 1) {
+    if (!mine) return;
+    const size_t at = (size_t)(job.part0 + split) * a.rows + row;
+    if (half == 0) a.ml[at] = f2{w.mx == -INFINITY ? w.mx : w.mx + a.offset, total};
+    if (t0 >= t1) return;
+#pragma unroll
+    for (int d = 0; d < DH / 32; d++)
+#pragma unroll
+      for (int e = 0; e < 4; e++)
+        *reinterpret_cast<f4*>(a.part + at * DH + 32 * d + 8 * e + 4 * half) = f4{w.o[d][4 * e], w.o[d][4 * e + 1], w.o[d][4 * e + 2], w.o[d][4 * e + 3]};
+    return;
+  }
+  if (idle) return;
+  if (a.lse && half == 0 && mine) a.lse[row] = live ? (w.mx == -INFINITY ? 0.f : w.mx) + a.offset + log2f(total) : INFINITY;
+  const bool sees = live && a.P + end > 0;
+  const float inv = 1.f / total;
+  unsigned char* Os = cache_smem + wave * 32 * S::KLD;  // (behind the last barrier nobody reads the tiles)
+#pragma unroll
+  for (int d = 0; d < DH / 32; d++)
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      const float y0 = sees ? w.o[d][2 * e] * inv : 0.f, y1 = sees ? w.o[d][2 * e + 1] * inv : 0.f;
+      *reinterpret_cast<uint32_t*>(Os + i * S::KLD + (32 * d + 8 * (e >> 1) + 4 * half + 2 * (e & 1)) * 2) = Mma<T>::head(y0, y1);
+    }
+  wave_lds_order();
+#pragma unroll
+  for (int j = 0; j < 32 * S::VEC / 64; j++) {
+    const int at = lane + 64 * j, rr = at / S::VEC, c = at % S::VEC, rt = tile * MROWS + wave * 32 + rr;
+    if (rt < job.rows)
+      *reinterpret_cast<u4*>(static_cast<T*>(a.O) + out_row(a, row_of(a, job, group, rt), DH) + 8 * c) = *reinterpret_cast<const u4*>(Os + rr * S::KLD + c * 16);
+  }
+}
+
+// Maximum and sum of a row over its parts, by a whole wavefront: lane s has part s, s + 64, ...
+__device__ inline void row_stats(const AttnArgs& a, int row, int lane, float& ref, float& total) {
+  float top = -INFINITY;
+  for (int s = lane; s < a.parts; s += 64) top = fmaxf(top, a.ml[(size_t)s * a.rows + row][0]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  ref = top == -INFINITY ? 0.f : top;
+  total = 0.f;
+  for (int s = lane; s < a.parts; s += 64) {
+    const f2 x = a.ml[(size_t)s * a.rows + row];
+    total += x[1] * exp2_fast(x[0] - ref);
+  }
+  total = wave_sum(total);
+}
+__device__ inline bool row_live(const AttnArgs& a, int row, bool& sees) {
   const int b = row / a.T / a.H, t = row % a.T;
   const int n = clamp_len(a.len[b], a.max_len), m = a.q_len ? clamp_len(a.q_len[b], a.T) : a.T;
-  const bool live = t < m && a.P + clamp_len(n - m + t + 1, n) > 0;
-  float top = -INFINITY;
-  for (int s = 0; s < a.parts; s++) top = fmaxf(top, a.ml[(size_t)s * a.rows + row][0]);
-  const float ref = top == -INFINITY ? 0.f : top;
-  float total = 0.f, v[DH / 64];
-#pragma unroll
-  for (int e = 0; e < DH / 64; e++) v[e] = 0.f;
-  for (int s = 0; s < a.parts; s++) {
+  sees = t < m && a.P + clamp_len(n - m + t + 1, n) > 0;
+  return t < m;
+}
+
+// The parts of rows joined.  A wavefront has a row; its lanes have four elements each and share the parts.
+template <typename T, int DH>
+__device__ inline void join_row(const AttnArgs& a, int row, int lane) {
+  constexpr int C = DH / 4, GR = 64 / C;  // lanes of an output, parts at a time
+  const int c = lane % C, p = lane / C;
+  float ref, total;
+  bool sees;
+  const bool live = row_live(a, row, sees);
+  row_stats(a, row, lane, ref, total);
+  f4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int s = p; s < a.parts; s += GR) {
     const f2 x = a.ml[(size_t)s * a.rows + row];
     if (x[0] == -INFINITY && x[1] == 0.f) continue;  // saw nothing: its part is not written
-    const float f = exp2_fast(x[0] - ref);
-    total += f * x[1];
-#pragma unroll
-    for (int e = 0; e < DH / 64; e++) v[e] += f * a.part[((size_t)s * a.rows + row) * DH + 64 * e + lane];
+    v += exp2_fast(x[0] - ref) * *reinterpret_cast<const f4*>(a.part + ((size_t)s * a.rows + row) * DH + 4 * c);
   }
-  T* out = static_cast<T*>(a.O) + out_row(a, row, DH) + lane;
 #pragma unroll
-  for (int e = 0; e < DH / 64; e++) out[64 * e] = Vec16<T>::round(live ? v[e] / total : 0.f);
+  for (int e = 0; e < 4; e++)
+#pragma unroll
+    for (int o = C; o < 64; o <<= 1) v[e] += __shfl_xor(v[e], o, 64);
+  if (p == 0) {
+    T* out = static_cast<T*>(a.O) + out_row(a, row, DH) + 4 * c;
+#pragma unroll
+    for (int e = 0; e < 4; e++) out[e] = Vec16<T>::round(sees ? v[e] / total : 0.f);
+  }
   if (a.lse && lane == 0) a.lse[row] = live ? ref + log2f(total) : INFINITY;
+}
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
+  const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row < a.rows) join_row<T, DH>(a, row, threadIdx.x & 63);
+}
+
+// Few rows: the parts joined, and what slots gather from the scores that were kept.  The first workgroups join rows, each of the others adds the
+// probabilities of a sequence's rows to GW slots of a head.
+constexpr int GW = 1024;
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void join_gather_kernel(AttnArgs a, int row_wgs, int chunks) {
+  __shared__ float lse[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if ((int)blockIdx.x < row_wgs) {
+    const int row = blockIdx.x * 4 + wave;
+    if (row < a.rows) join_row<T, DH>(a, row, lane);
+    return;
+  }
+  const unsigned item = blockIdx.x - row_wgs, bh = item / chunks;
+  const int b = bh / a.Hk, first = (int)(item % chunks) * GW, n = clamp_len(a.len[b], a.max_len);
+  if (first >= n) return;
+  for (int r = wave; r < a.R; r += 4) {
+    const int row = bh * a.R + r;
+    float ref, total;
+    bool sees;
+    const bool live = row_live(a, row, sees);
+    if (a.parts > 1) {
+      row_stats(a, row, lane, ref, total);
+      ref += log2f(total);
+    } else {
+      ref = a.lse[row];
+    }
+    if (lane == 0) lse[r] = live ? ref : INFINITY;
+  }
+  __syncthreads();
+  const int k = first + 4 * (int)threadIdx.x;
+  if (k >= n) return;
+  float* w = a.weight + (size_t)bh * a.cap + k;
+  f4 acc = {0.f, 0.f, 0.f, 0.f};
+  const int m = a.q_len ? clamp_len(a.q_len[b], a.T) : a.T;
+#pragma unroll 4
+  for (int r = 0; r < a.R; r++) {
+    // a row's scores are there up to the tile that its group's last row sees; behind what the row sees they are not looked at
+    const int end = seen(a, r, n, m);
+    f4 s = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    if (k < end && lse[r] < INFINITY) s = *reinterpret_cast<const f4*>(a.score + (size_t)(bh * a.R + r) * a.score_ld + k);
+#pragma unroll
+    for (int e = 0; e < 4; e++) acc[e] += k + e < end && lse[r] < INFINITY ? exp2_fast(s[e] - lse[r]) : 0.f;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; e++)
+    if (k + e < n) w[e] += acc[e];
 }
 
 // What slots gather: 16 keys per wavefront, kept in registers; the rows of queries pass by, 16 at a time.
@@ -457,13 +794,15 @@ __global__ __launch_bounds__(256) void gather_kernel(AttnArgs a, int chunks) {
 
 // How a call is cut.  The prefix of an image's sequences is read once for all of them where the rows of one sequence do not fill a
 // tile by themselves; else a sequence's rows go over its prefix and its cache in one sweep.
-constexpr int FEW_WG = 1024, FEW_ROWS = 16;
-static Job make_job(int groups, int rows, int keys, bool packed, bool prefix, bool cache) {
-  Job j = {groups, rows, (rows + FEW_ROWS - 1) / FEW_ROWS, 1, 0, packed, prefix, cache};
-  // parts of the keys: enough workgroups for the chip, and a tile for each wavefront
-  const long long items = (long long)groups * j.tiles, tiles = (keys + FK - 1) / FK + (prefix && cache ? 1 : 0);
-  long long s = (FEW_WG + items - 1) / items;
-  if (s > (tiles + 3) / 4) s = (tiles + 3) / 4;
+constexpr int FEW_WG = 1024, FEW_ROWS = 16, MANY_WG = 512;
+static Job make_job(const CachePlan& pl, int groups, int rows, int keys, bool packed, bool prefix, bool cache) {
+  const bool many = rows > FEW_ROWS && pl.esize == 2;
+  const int per = many ? MROWS : FEW_ROWS, tile = many ? MK : FK, least = many ? 2 : 4, want = many ? MANY_WG : FEW_WG;
+  Job j = {groups, rows, (rows + per - 1) / per, 1, 0, packed, prefix, cache, many};
+  // parts of the keys: enough workgroups for the chip, and `least` tiles for each
+  const long long items = (long long)groups * j.tiles, tiles = (keys + tile - 1) / tile + (prefix && cache ? 1 : 0);
+  long long s = (want + items - 1) / items;
+  if (s > (tiles + least - 1) / least) s = (tiles + least - 1) / least;
   j.splits = s < 1 ? 1 : (int)s;
   return j;
 }
@@ -476,13 +815,13 @@ static Cut make_cut(const CachePlan& pl, int max_len) {
   Cut c = {};
   if (pl.images > 0 && pl.each > 1 && pl.R < 128) {
     c.jobs = 2;
-    c.job[0] = make_job(pl.images * pl.Hk, pl.each * pl.R, pl.P, true, true, false);
-    c.job[1] = make_job(pl.B * pl.Hk, pl.R, max_len, false, false, true);
+    c.job[0] = make_job(pl, pl.images * pl.Hk, pl.each * pl.R, pl.P, true, true, false);
+    c.job[1] = make_job(pl, pl.B * pl.Hk, pl.R, max_len, false, false, true);
     c.job[1].part0 = c.job[0].splits;
     c.parts = c.job[0].splits + c.job[1].splits;
   } else {
     c.jobs = 1;
-    c.job[0] = make_job(pl.B * pl.Hk, pl.R, pl.P + max_len, false, pl.P > 0, true);
+    c.job[0] = make_job(pl, pl.B * pl.Hk, pl.R, pl.P + max_len, false, pl.P > 0, true);
     c.parts = c.job[0].splits;
   }
   return c;
@@ -494,23 +833,54 @@ static size_t part_rows(const CachePlan& pl) {
   const Cut c = make_cut(pl, pl.cap);  // (longer caches are cut into no fewer parts)
   return c.parts > 1 ? (size_t)pl.B * pl.H * pl.T * c.parts : 0;
 }
-size_t attention_bytes(const CachePlan& pl) {
-  return align256((size_t)pl.B * pl.H * pl.T * 4) + align256(part_rows(pl) * 8) + part_rows(pl) * pl.dh * 4;
+// Few rows of a sequence: their scores are kept, so that the keys are read once.
+static bool keeps_scores(const CachePlan& pl) { return pl.R <= FEW_ROWS; }
+static int score_ld(int max_len) { return round_up(max_len, FK); }
+static size_t score_elems(const CachePlan& pl) {
+  return keeps_scores(pl) ? (size_t)pl.B * pl.H * pl.T * score_ld(pl.cap) : 0;
 }
+size_t attention_bytes(const CachePlan& pl) {
+  return align256((size_t)pl.B * pl.H * pl.T * 4) + align256(part_rows(pl) * 8) + align256(score_elems(pl) * 4) + part_rows(pl) * pl.dh * 4;
+}
+
+template <typename K>
+static bool allow_lds(K kernel, int bytes) {  // (and up to 1 KB that the kernels declare)
+  return bytes + 1024 <= 64 * 1024 ||
+         hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess;
+}
+static long long workgroups(const Job& j) { return (long long)j.groups * j.tiles * j.splits; }
 
 template <typename T, int DH>
 static int attention_launch(const CachePlan& pl, AttnArgs a, hipStream_t st) {
-  typedef FewShape<T, DH> S;
   const Cut cut = make_cut(pl, pl.max_len);
   a.parts = cut.parts;
-  long long grid = 0, chunks = (pl.max_len + 63) / 64;
-  for (int k = 0; k < cut.jobs; k++) grid += (long long)cut.job[k].groups * cut.job[k].tiles * cut.job[k].splits;
-  if (grid > 0x7fffffffLL || (a.weight && chunks * pl.B * pl.Hk > 0x7fffffffLL)) return TC_ERR_SHAPE;
-  if (S::LDS + 1024 > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(few_kernel<T, DH>),
-                                                       hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS) != hipSuccess)
-    return TC_ERR_HIP;
-  few_kernel<T, DH><<<(unsigned)grid, 256, S::LDS, st>>>(a, cut.job[0], cut.job[cut.jobs - 1]);
-  if (a.parts > 1) join_kernel<T, DH><<<(a.rows + 3) / 4, 256, 0, st>>>(a);
+  long long chunks = (pl.max_len + 63) / 64;
+  if (workgroups(cut.job[0]) + workgroups(cut.job[1]) > 0x7fffffffLL || (a.weight && chunks * pl.B * pl.Hk > 0x7fffffffLL)) return TC_ERR_SHAPE;
+  Job few[2] = {};
+  int nf = 0;
+  for (int k = 0; k < cut.jobs; k++) {
+    if (!cut.job[k].many) {
+      few[nf++] = cut.job[k];
+      continue;
+    }
+    if constexpr (sizeof(T) == 2) {
+      if (!allow_lds(many_kernel<T, DH>, ManyShape<DH>::LDS)) return TC_ERR_HIP;
+      many_kernel<T, DH><<<(unsigned)workgroups(cut.job[k]), 256, ManyShape<DH>::LDS, st>>>(a, cut.job[k]);
+    }
+  }
+  if (nf > 0) {
+    if (!allow_lds(few_kernel<T, DH>, FewShape<T, DH>::LDS)) return TC_ERR_HIP;
+    few_kernel<T, DH><<<(unsigned)(workgroups(few[0]) + workgroups(few[1])), 256, FewShape<T, DH>::LDS, st>>>(a, few[0], few[1]);
+  }
+  const int row_wgs = a.parts > 1 ? (a.rows + 3) / 4 : 0;
+  if (a.weight && a.score) {
+    chunks = (pl.max_len + GW - 1) / GW;
+    const long long wgs = row_wgs + chunks * pl.B * pl.Hk;
+    if (wgs > 0x7fffffffLL) return TC_ERR_SHAPE;
+    join_gather_kernel<T, DH><<<(unsigned)wgs, 256, 0, st>>>(a, row_wgs, (int)chunks);
+    return check_launch();
+  }
+  if (a.parts > 1) join_kernel<T, DH><<<row_wgs, 256, 0, st>>>(a);
   if (a.weight) gather_kernel<T, DH><<<(unsigned)(chunks * pl.B * pl.Hk), 256, 0, st>>>(a, (int)chunks);
   return check_launch();
 }
@@ -538,12 +908,15 @@ extern "C" int tc_cache_attention(const tc_cache* c, const void* Q, const void* 
   a.scale2 = pl.scale * 1.44269504088896340736f;
   int bits = 1;  // 2^bits is more than twice the keys of a row
   while ((1LL << bits) <= 2LL * pl.P + 2LL * pl.max_len) bits++;
-  a.offset = c->dtype == TC_F16 ? 0.f : (float)bits;  // (half: its values times float32 sums are far from that range, and small halves lose bits)
+  a.offset = c->dtype == TC_F16 ? 0.f : bits + LAZY;  // (half: its values times float32 sums are far from that range, and small halves lose bits)
   char* w = static_cast<char*>(ws);
   a.lse = weight ? reinterpret_cast<float*>(w) : nullptr;
   w += align256((size_t)a.rows * 4);
   a.ml = reinterpret_cast<f2*>(w);
   w += align256(part_rows(pl) * 8);
+  a.score = weight && keeps_scores(pl) ? reinterpret_cast<float*>(w) : nullptr;
+  a.score_ld = score_ld(pl.max_len);
+  w += align256(score_elems(pl) * 4);
   a.part = reinterpret_cast<float*>(w);
   const hipStream_t st = (hipStream_t)stream;
   if (pl.dh == 64)

@@ -44,7 +44,8 @@ def call(s):
 
 def check(s, before=None):
     """Runs the call and compares.  The bound of an output, A = sum p |v| of its row:
-      half a step of the storage type of O; of the probabilities too, where they enter the products rounded once (times A);
+      half a step of the storage type of O; of the probabilities too, where they enter the products rounded once (p (1 + e), |e| <= h each: off
+      by h A at most), which they do in tiles of more than 16 rows: those of a sequence, or of all sequences of an image at its prefix;
       scores: d + 4 roundings of float32 of at most scale sum |q k|, in the exponent, so relative to p, numerator and sum: twice;
       2^-20 for the exponentials (an ulp or two each) and sums; half storage: probabilities below its normal numbers, 2^-25 each."""
     _, orc = _tc()
@@ -69,7 +70,8 @@ def check(s, before=None):
         es = 0.0 if keys.shape[1] == 0 or m == 0 else 2.0 ** -24 * (d + 4) * scale * max(
             np.abs(host["Q"][b, x, :m]).dot(np.abs(keys[x // (H // Hk)]).T).max() for x in range(H))
         rel = 2 * (es + 2.0 ** -20)
-        bound = h * np.abs(want) + ((h if H // Hk * T > 16 else h * h) if sixteen else 0) * A + rel * A
+        tile = H // Hk * T * (B // c.n_prefixes if c.prefix_len else 1)
+        bound = h * np.abs(want) + ((h if tile > 16 else h * h) if sixteen else 0) * A + rel * A
         if sd == torch.float16 and keys.shape[1]:
             bound = bound + 2.0 ** -25 * (1 + np.abs(vals).sum(1).max())
         got = host["O"][b].reshape(T, H, d)
