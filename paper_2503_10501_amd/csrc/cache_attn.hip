@@ -149,11 +149,20 @@ __device__ inline bool not_finite(T v) {
   else if constexpr (Mma<T>::WIDE) return (v & 0x7f80u) == 0x7f80u;
   else return (__builtin_bit_cast(uint16_t, v) & 0x7c00u) == 0x7c00u;
 }
-// two packed values, those that are not finite as zero
+// A vector's values, those that are not finite as zero.
 template <typename T>
-__device__ inline uint32_t finite_only(uint32_t w) {
-  return (not_finite<T>(__builtin_bit_cast(T, (uint16_t)w)) ? 0 : w & 0xffffu) |
-         (not_finite<T>(__builtin_bit_cast(T, (uint16_t)(w >> 16))) ? 0 : w & 0xffff0000u);
+__device__ inline u4 finite_only(u4 w) {
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const uint32_t x = w[i];
+    if constexpr (sizeof(T) == 4) {
+      if ((x & 0x7f800000u) == 0x7f800000u) w[i] = 0;
+    } else {
+      constexpr uint32_t E = Mma<T>::WIDE ? 0x7f80u : 0x7c00u;
+      w[i] = ((x & E) == E ? 0 : x & 0xffffu) | ((x & E << 16) == E << 16 ? 0 : x & 0xffff0000u);
+    }
+  }
+  return w;
 }
 template <typename T>
 __device__ inline bool any_not_finite(const u4& w) {
@@ -169,6 +178,27 @@ __device__ inline bool any_not_finite(const u4& w) {
     }
   }
   return bad;
+}
+
+// Rows of keys and values from `first` on to registers, N threads side by side: they are one run of 16-byte vectors.  Behind the `there` rows
+// that exist the last vector of these is read; of values zero stands in its place (zero_behind) before they are used.
+template <int N, int VEC, int NV>
+__device__ __forceinline__ void fetch_tile(const void* K, const void* V, size_t first, int there, int id, u4 (&kr)[NV], u4 (&vr)[NV]) {
+  const char* Kb = static_cast<const char*>(K) + first * VEC * 16;
+  const char* Vb = static_cast<const char*>(V) + first * VEC * 16;
+  const int end = min(there, N * NV / VEC) * VEC - 1;
+#pragma unroll
+  for (int j = 0; j < NV; j++) {
+    const unsigned off = (unsigned)min(id + N * j, end) * 16;
+    kr[j] = *reinterpret_cast<const u4*>(Kb + off);
+    vr[j] = *reinterpret_cast<const u4*>(Vb + off);
+  }
+}
+template <int N, int VEC, int NV>
+__device__ __forceinline__ void zero_behind(int there, int id, u4 (&vr)[NV]) {
+#pragma unroll
+  for (int j = 0; j < NV; j++)
+    if (id + N * j >= there * VEC) vr[j] = u4{0, 0, 0, 0};
 }
 
 // ---- few rows: one workgroup has 16 rows, its four wavefronts share the keys, 32 at a time, without waiting for one another ----
@@ -224,19 +254,10 @@ __global__ __launch_bounds__(256) void few_kernel(AttnArgs a, Job first, Job sec
   unsigned char* Ks = cache_smem + wave * S::WAVE;
   unsigned char* Vs = Ks + FK * S::KLD;
   u4 kr[NV], vr[NV];
-  // a tile comes through registers: rows behind the last key are read as the last one, and their values as zero
   auto fetch = [&](int t) {
     const bool pre = t < np;
-    const int k0 = (pre ? t : t - np) * FK, last = (pre ? a.P : most) - 1;
-    const u4* K = reinterpret_cast<const u4*>(static_cast<const T*>(pre ? a.Kp : a.Kc) + (pre ? phead : head) * DH);
-    const u4* V = reinterpret_cast<const u4*>(static_cast<const T*>(pre ? a.Vp : a.Vc) + (pre ? phead : head) * DH);
-#pragma unroll
-    for (int j = 0; j < NV; j++) {
-      const int at = lane + 64 * j, key = k0 + at / VEC;
-      kr[j] = K[(size_t)min(key, last) * VEC + at % VEC];
-      const u4 v = V[(size_t)min(key, last) * VEC + at % VEC];
-      vr[j] = key <= last ? v : u4{0, 0, 0, 0};
-    }
+    const int k0 = (pre ? t : t - np) * FK;
+    fetch_tile<64, VEC>(pre ? a.Kp : a.Kc, pre ? a.Vp : a.Vc, (pre ? phead : head) + k0, (pre ? a.P : most) - k0, lane, kr, vr);
   };
 
   frag q[DH / 32];
@@ -258,10 +279,15 @@ __global__ __launch_bounds__(256) void few_kernel(AttnArgs a, Job first, Job sec
     const bool masked = k0 + FK > (pre ? a.P : least);  // some row does not see some key
     bool odd = false;                                    // a value that is not finite where rows differ in what they see
     if (masked) {
+      zero_behind<64, VEC>(last - k0, lane, vr);
 #pragma unroll
       for (int j = 0; j < NV; j++) odd |= any_not_finite<T>(vr[j]);
+      odd = __ballot(odd) != 0;
+      if (odd) {
+#pragma unroll
+        for (int j = 0; j < NV; j++) vr[j] = finite_only<T>(vr[j]);
+      }
     }
-    odd = __ballot(odd) != 0;
 #pragma unroll
     for (int j = 0; j < NV; j++) {
       const int at = lane + 64 * j, key = at / VEC, c = at % VEC;
@@ -332,29 +358,21 @@ __global__ __launch_bounds__(256) void few_kernel(AttnArgs a, Job first, Job sec
           v.h[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)at);
         }
       }
-      if (odd) {
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-          for (int j = 0; j < 8; j++) v.f[j] = not_finite(v.f[j]) ? 0.f : v.f[j];
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; j++) v.w[j] = finite_only<T>(v.w[j]);
-        }
-      }
       o[d] = M::mul(v, ph, o[d]);
       if constexpr (sizeof(T) == 2) o[d] = M::mul(v, pr, o[d]);
     }
-    if (odd) {  // values that are not finite reach the rows that see them, and no other
-      for (int k = 0; k < FK; k++) {
-        if (k0 + k >= (pre ? last : end)) continue;
+    if (odd) {  // these reach the rows that see them, and no other
+      const T* V = static_cast<const T*>(pre ? a.Vp : a.Vc) + ((pre ? phead : head) + k0) * DH;
+      const int keys = min(FK, last - k0), lim = (pre ? last : end) - k0;
+#pragma unroll 1
+      for (int k = 0; k < keys; k++)
 #pragma unroll
         for (int d = 0; d < DT; d++)
 #pragma unroll
           for (int e = 0; e < 4; e++) {
-            const T v = *reinterpret_cast<const T*>(Vs + k * S::VLD + (16 * d + 4 * g + e) * ES);
-            if (not_finite(v)) o[d][e] += Vec16<T>::one(v);
+            const T v = V[(size_t)k * DH + 16 * d + 4 * g + e];
+            if (k < lim && not_finite(v)) o[d][e] += Vec16<T>::one(v);
           }
-      }
     }
     wave_lds_order();
   }
@@ -427,9 +445,9 @@ struct ManyWave {
   f16v o[DH / 32];
   float mx, sum;
 
-  // One tile.  MASKED: some row of the wavefront does not see some key; keys below `lim` are seen by this lane's row.
-  template <bool MASKED>
-  __device__ __forceinline__ void step(const unsigned char* Ks, const unsigned char* Vs, int k0, int lim, bool odd, float scale2, float offset,
+  // One tile.  `masked`: some row of the wavefront does not see some key; keys below `lim` are seen by this lane's row.  (One body for both: with
+  // two the partial output would move between registers.)
+  __device__ __forceinline__ void step(const unsigned char* Ks, const unsigned char* Vs, int k0, int lim, bool masked, float scale2, float offset,
                                        int lane) {
     const int half = lane >> 5, i = lane & 31;
     f16v s[2];
@@ -444,7 +462,7 @@ struct ManyWave {
         k.u = *reinterpret_cast<const u4*>(kr + u * 32 * S::KLD + 32 * c);
         s[u] = M::mul32(k, q[c], s[u]);
       }
-    if (MASKED) {
+    if (masked) {
 #pragma unroll
       for (int u = 0; u < 2; u++)
 #pragma unroll
@@ -489,26 +507,23 @@ struct ManyWave {
             const unsigned char* at = Vs + (32 * u + 16 * v + 8 * j + 4 * half + (i & 15) / 4) * S::VLD + (32 * d + (i & 16) + 4 * (i & 3)) * 2;
             x.h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4v*)const_cast<unsigned char*>(at));
           }
-          if (MASKED && odd) {
-#pragma unroll
-            for (int j = 0; j < 4; j++) x.w[j] = finite_only<T>(x.w[j]);
-          }
           o[d] = M::mul32(x, ph, o[d]);
         }
       }
     }
-    if (MASKED && odd) {  // values that are not finite reach the rows that see them, and no other
-      for (int k = 0; k < MK; k++) {
-        if (k0 + k >= lim) continue;
+  }
+
+  // Values that are not finite, which the tile has zero for, reach the rows that see them, and no other.
+  __device__ __forceinline__ void add_odd(const T* V, int keys, int lim, int lane) {
+#pragma unroll 1
+    for (int k = 0; k < keys; k++)
 #pragma unroll
-        for (int d = 0; d < DH / 32; d++)
+      for (int d = 0; d < DH / 32; d++)
 #pragma unroll
-          for (int e = 0; e < 16; e++) {
-            const T v = *reinterpret_cast<const T*>(Vs + k * S::VLD + (32 * d + 8 * (e >> 2) + 4 * half + (e & 3)) * 2);
-            if (not_finite(v)) o[d][e] += Vec16<T>::one(v);
-          }
-      }
-    }
+        for (int e = 0; e < 16; e++) {
+          const T v = V[(size_t)k * DH + 32 * d + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)];
+          if (k < lim && not_finite(v)) o[d][e] += Vec16<T>::one(v);
+        }
   }
 };
 
@@ -518,6 +533,7 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
   typedef ManyWave<T, DH> Wave;
   extern __shared__ __attribute__((aligned(16))) unsigned char cache_smem[];
   __shared__ int ends[2][4], flag[3];
+  __shared__ size_t places[4][32];  // of rows in the output
   int group, item;
   if (!group_on_xcd(blockIdx.x, job.tiles * job.splits, job.groups, &group, &item)) return;
   const int split = item % job.splits, tile = job.tiles - 1 - item / job.splits;  // (the rows that see the most first)
@@ -553,29 +569,26 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
 
   const size_t head = (size_t)group * a.cap, phead = job.prefix ? ((size_t)(job.packed ? b : b / a.each) * a.Hk + hk) * a.P : 0;
   u4 kr[S::NV], vr[S::NV];
-  // rows behind the last key are read as the last one, and their values as zero
   auto fetch = [&](int t) {
     const bool pre = t < np;
-    const int k0 = (pre ? t : t - np) * MK, last = (pre ? a.P : most) - 1;
-    const u4* K = reinterpret_cast<const u4*>(static_cast<const T*>(pre ? a.Kp : a.Kc) + (pre ? phead : head) * DH);
-    const u4* V = reinterpret_cast<const u4*>(static_cast<const T*>(pre ? a.Vp : a.Vc) + (pre ? phead : head) * DH);
-#pragma unroll
-    for (int j = 0; j < S::NV; j++) {
-      const int at = tid + 256 * j, key = k0 + at / S::VEC;
-      kr[j] = K[(size_t)min(key, last) * S::VEC + at % S::VEC];
-      const u4 v = V[(size_t)min(key, last) * S::VEC + at % S::VEC];
-      vr[j] = key <= last ? v : u4{0, 0, 0, 0};
-    }
+    const int k0 = (pre ? t : t - np) * MK;
+    fetch_tile<256, S::VEC>(pre ? a.Kp : a.Kc, pre ? a.Vp : a.Vc, (pre ? phead : head) + k0, (pre ? a.P : most) - k0, tid, kr, vr);
   };
   auto store = [&](int t) {
     unsigned char* Ks = cache_smem + (t & 1) * S::STAGE;
     unsigned char* Vs = Ks + MK * S::KLD;
     const bool pre = t < np;
-    if ((pre ? t : t - np) * MK + MK > (pre ? a.P : least)) {  // rows differ in what they see: is every value finite?
+    const int k0 = (pre ? t : t - np) * MK;
+    if (k0 + MK > (pre ? a.P : least)) {  // rows differ in what they see: is every value finite?
       bool odd = false;
+      zero_behind<256, S::VEC>((pre ? a.P : most) - k0, tid, vr);
 #pragma unroll
       for (int j = 0; j < S::NV; j++) odd |= any_not_finite<T>(vr[j]);
-      if (odd) flag[t % 3] = 1;
+      if (odd) {
+        flag[t % 3] = 1;
+#pragma unroll
+        for (int j = 0; j < S::NV; j++) vr[j] = finite_only<T>(vr[j]);
+      }
     }
 #pragma unroll
     for (int j = 0; j < S::NV; j++) {
@@ -608,10 +621,10 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
     const int k0 = (pre ? t : t - np) * MK, lim = pre ? a.P : end;
     const unsigned char* Ks = cache_smem + (t & 1) * S::STAGE;
     if (!idle && (pre || k0 < wave_most)) {
-      if (k0 + MK > (pre ? a.P : wave_least))
-        w.template step<true>(Ks, Ks + MK * S::KLD, k0, lim, flag[t % 3] != 0, a.scale2, a.offset, lane);
-      else
-        w.template step<false>(Ks, Ks + MK * S::KLD, k0, lim, false, a.scale2, a.offset, lane);
+      const bool masked = k0 + MK > (pre ? a.P : wave_least);
+      w.step(Ks, Ks + MK * S::KLD, k0, lim, masked, a.scale2, a.offset, lane);
+      if (masked && __builtin_amdgcn_readfirstlane(flag[t % 3]))
+        w.add_odd(static_cast<const T*>(pre ? a.Vp : a.Vc) + ((pre ? phead : head) + k0) * DH, min(MK, (pre ? a.P : most) - k0), lim - k0, lane);
     }
     if (tid == 0) flag[(t + 2) % 3] = 0;  // (last looked at before the last barrier, set again behind the next one)
     if (t + 1 < t1) store(t + 1);         // the other stage was last read before the last barrier
@@ -637,6 +650,7 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
   const bool sees = live && a.P + end > 0;
   const float inv = 1.f / total;
   unsigned char* Os = cache_smem + wave * 32 * S::KLD;  // (behind the last barrier nobody reads the tiles)
+  if (half == 0) places[wave][i] = out_row(a, row, DH);
 #pragma unroll
   for (int d = 0; d < DH / 32; d++)
 #pragma unroll
@@ -647,9 +661,9 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
   wave_lds_order();
 #pragma unroll
   for (int j = 0; j < 32 * S::VEC / 64; j++) {
-    const int at = lane + 64 * j, rr = at / S::VEC, c = at % S::VEC, rt = tile * MROWS + wave * 32 + rr;
-    if (rt < job.rows)
-      *reinterpret_cast<u4*>(static_cast<T*>(a.O) + out_row(a, row_of(a, job, group, rt), DH) + 8 * c) = *reinterpret_cast<const u4*>(Os + rr * S::KLD + c * 16);
+    const int at = lane + 64 * j, rr = at / S::VEC, c = at % S::VEC;
+    if (tile * MROWS + wave * 32 + rr < job.rows)
+      *reinterpret_cast<u4*>(static_cast<T*>(a.O) + places[wave][rr] + 8 * c) = *reinterpret_cast<const u4*>(Os + rr * S::KLD + c * 16);
   }
 }
 
@@ -844,8 +858,8 @@ size_t attention_bytes(const CachePlan& pl) {
 }
 
 template <typename K>
-static bool allow_lds(K kernel, int bytes) {  // (and up to 1 KB that the kernels declare)
-  return bytes + 1024 <= 64 * 1024 ||
+static bool allow_lds(K kernel, int bytes) {  // (and up to 2 KB that the kernels declare)
+  return bytes + 2048 <= 64 * 1024 ||
          hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess;
 }
 static long long workgroups(const Job& j) { return (long long)j.groups * j.tiles * j.splits; }
