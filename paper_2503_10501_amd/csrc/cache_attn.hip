@@ -213,7 +213,9 @@ struct FewShape {
   static_assert(16 * (DH + 4) * 4 <= WAVE, "the partial output takes the place of the tiles");
 };
 
-template <typename T, int DH>
+// KEEP: scores of the cache's keys are written.  Unconditionally, so that the count of accesses in flight is known and a tile's loads need not wait
+// for them: lanes behind the last row have its scores, and scores of a prefix go to FK places behind a row's own.
+template <typename T, int DH, bool KEEP>
 __global__ __launch_bounds__(256) void few_kernel(AttnArgs a, Job first, Job second) {
   typedef FewShape<T, DH> S;
   typedef Mma<T> M;
@@ -312,9 +314,10 @@ __global__ __launch_bounds__(256) void few_kernel(AttnArgs a, Job first, Job sec
         s[u][e] = !masked || key < (pre ? last : end) ? s[u][e] * a.scale2 : -INFINITY;
         top = fmaxf(top, s[u][e]);
       }
-    if (a.score && !pre && mine) {
+    if (KEEP) {
+      float* to = a.score + (size_t)row * a.score_ld + (pre ? a.score_ld - FK : k0) + 4 * g;
 #pragma unroll
-      for (int u = 0; u < 2; u++) *reinterpret_cast<f4*>(a.score + (size_t)row * a.score_ld + k0 + 16 * u + 4 * g) = s[u];
+      for (int u = 0; u < 2; u++) *reinterpret_cast<f4*>(to + 16 * u) = s[u];
     }
     top = fmaxf(mx, col_max(top));
     const float ref = top == -INFINITY ? 0.f : top + a.offset;
@@ -688,11 +691,12 @@ __device__ inline bool row_live(const AttnArgs& a, int row, bool& sees) {
   return t < m;
 }
 
-// The parts of rows joined.  A wavefront has a row; its lanes have four elements each and share the parts.
-template <typename T, int DH>
-__device__ inline void join_row(const AttnArgs& a, int row, int lane) {
-  constexpr int C = DH / 4, GR = 64 / C;  // lanes of an output, parts at a time
-  const int c = lane % C, p = lane / C;
+// The parts of a row joined by a wavefront (ROW_WAVES = 1) or, where they are many, by a workgroup: a lane has four elements of every
+// ROW_WAVES 256 / d_h -th part.  (One sequence of 32768 keys, 32 rows of 128 parts: 37 us by a wavefront each, 8 by a workgroup.)
+template <typename T, int DH, int ROW_WAVES>
+__device__ inline void join_row(const AttnArgs& a, int row, float* lds) {
+  constexpr int C = DH / 4, GR = ROW_WAVES * 64 / C;  // lanes of an output, parts at a time
+  const int id = threadIdx.x % (ROW_WAVES * 64), lane = id & 63, c = id % C, p = id / C;
   float ref, total;
   bool sees;
   const bool live = row_live(a, row, sees);
@@ -708,17 +712,39 @@ __device__ inline void join_row(const AttnArgs& a, int row, int lane) {
   for (int e = 0; e < 4; e++)
 #pragma unroll
     for (int o = C; o < 64; o <<= 1) v[e] += __shfl_xor(v[e], o, 64);
+  if constexpr (ROW_WAVES > 1) {
+    f4* part = reinterpret_cast<f4*>(lds);  // [wavefront][C]
+    if (lane < C) part[id / 64 * C + lane] = v;
+    __syncthreads();
+    if (id < C) {
+      v = part[id];
+#pragma unroll
+      for (int w = 1; w < ROW_WAVES; w++) v += part[w * C + id];
+    }
+  }
   if (p == 0) {
     T* out = static_cast<T*>(a.O) + out_row(a, row, DH) + 4 * c;
 #pragma unroll
     for (int e = 0; e < 4; e++) out[e] = Vec16<T>::round(sees ? v[e] / total : 0.f);
   }
-  if (a.lse && lane == 0) a.lse[row] = live ? ref + log2f(total) : INFINITY;
+  if (a.lse && id == 0) a.lse[row] = live ? ref + log2f(total) : INFINITY;
 }
+constexpr int WIDE_JOIN = 9;  // parts from which on a workgroup joins a row
+template <typename T, int DH>
+__device__ inline void join_rows(const AttnArgs& a, float* lds) {
+  if (a.parts >= WIDE_JOIN) {
+    join_row<T, DH, 4>(a, blockIdx.x, lds);
+  } else {
+    const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row < a.rows) join_row<T, DH, 1>(a, row, lds);
+  }
+}
+inline int join_workgroups(const AttnArgs& a) { return a.parts >= WIDE_JOIN ? a.rows : a.parts > 1 ? (a.rows + 3) / 4 : 0; }
+
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
-  const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row < a.rows) join_row<T, DH>(a, row, threadIdx.x & 63);
+  __shared__ __attribute__((aligned(16))) float lds[4 * DH];
+  join_rows<T, DH>(a, lds);
 }
 
 // Few rows: the parts joined, and what slots gather from the scores that were kept.  The first workgroups join rows, each of the others adds the
@@ -727,10 +753,10 @@ constexpr int GW = 1024;
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void join_gather_kernel(AttnArgs a, int row_wgs, int chunks) {
   __shared__ float lse[16];
+  __shared__ __attribute__((aligned(16))) float lds[4 * DH];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if ((int)blockIdx.x < row_wgs) {
-    const int row = blockIdx.x * 4 + wave;
-    if (row < a.rows) join_row<T, DH>(a, row, lane);
+    join_rows<T, DH>(a, lds);
     return;
   }
   const unsigned item = blockIdx.x - row_wgs, bh = item / chunks;
@@ -808,15 +834,22 @@ __global__ __launch_bounds__(256) void gather_kernel(AttnArgs a, int chunks) {
 
 // How a call is cut.  The prefix of an image's sequences is read once for all of them where the rows of one sequence do not fill a
 // tile by themselves; else a sequence's rows go over its prefix and its cache in one sweep.
-constexpr int FEW_WG = 1024, FEW_ROWS = 16, MANY_WG = 512;
+constexpr int FEW_ROWS = 16;
 static Job make_job(const CachePlan& pl, int groups, int rows, int keys, bool packed, bool prefix, bool cache) {
   const bool many = rows > FEW_ROWS && pl.esize == 2;
-  const int per = many ? MROWS : FEW_ROWS, tile = many ? MK : FK, least = many ? 2 : 4, want = many ? MANY_WG : FEW_WG;
+  const int per = many ? MROWS : FEW_ROWS, tile = many ? MK : FK, least = many ? 2 : 4;
   Job j = {groups, rows, (rows + per - 1) / per, 1, 0, packed, prefix, cache, many};
-  // parts of the keys: enough workgroups for the chip, and `least` tiles for each
+  // Parts of the keys: two workgroups for each compute unit, if there is a tile for each wavefront (many: two for the workgroup).  Few rows
+  // of long caches take four of them, which evens out sequences of different lengths, where a wavefront still has four tiles.  (us, two and
+  // four: 4 sequences of up to 32768 keys 99 and 94; one 24 and 29; 64 sequences sharing 8 prefixes of 640 keys 52 and 57.)
   const long long items = (long long)groups * j.tiles, tiles = (keys + tile - 1) / tile + (prefix && cache ? 1 : 0);
-  long long s = (want + items - 1) / items;
+  long long s = (512 + items - 1) / items;
   if (s > (tiles + least - 1) / least) s = (tiles + least - 1) / least;
+  if (!many) {
+    long long t = (1024 + items - 1) / items;
+    if (t > tiles / 16) t = tiles / 16;
+    if (t > s) s = t;
+  }
   j.splits = s < 1 ? 1 : (int)s;
   return j;
 }
@@ -827,7 +860,7 @@ struct Cut {
 };
 static Cut make_cut(const CachePlan& pl, int max_len) {
   Cut c = {};
-  if (pl.images > 0 && pl.each > 1 && pl.R < 128) {
+  if (pl.images > 0 && pl.each > 1 && pl.R <= FEW_ROWS) {
     c.jobs = 2;
     c.job[0] = make_job(pl, pl.images * pl.Hk, pl.each * pl.R, pl.P, true, true, false);
     c.job[1] = make_job(pl, pl.B * pl.Hk, pl.R, max_len, false, false, true);
@@ -849,7 +882,7 @@ static size_t part_rows(const CachePlan& pl) {
 }
 // Few rows of a sequence: their scores are kept, so that the keys are read once.
 static bool keeps_scores(const CachePlan& pl) { return pl.R <= FEW_ROWS; }
-static int score_ld(int max_len) { return round_up(max_len, FK); }
+static int score_ld(int max_len) { return round_up(max_len, FK) + FK; }
 static size_t score_elems(const CachePlan& pl) {
   return keeps_scores(pl) ? (size_t)pl.B * pl.H * pl.T * score_ld(pl.cap) : 0;
 }
@@ -883,10 +916,11 @@ static int attention_launch(const CachePlan& pl, AttnArgs a, hipStream_t st) {
     }
   }
   if (nf > 0) {
-    if (!allow_lds(few_kernel<T, DH>, FewShape<T, DH>::LDS)) return TC_ERR_HIP;
-    few_kernel<T, DH><<<(unsigned)(workgroups(few[0]) + workgroups(few[1])), 256, FewShape<T, DH>::LDS, st>>>(a, few[0], few[1]);
+    const auto kernel = a.score ? few_kernel<T, DH, true> : few_kernel<T, DH, false>;
+    if (!allow_lds(kernel, FewShape<T, DH>::LDS)) return TC_ERR_HIP;
+    kernel<<<(unsigned)(workgroups(few[0]) + workgroups(few[1])), 256, FewShape<T, DH>::LDS, st>>>(a, few[0], few[1]);
   }
-  const int row_wgs = a.parts > 1 ? (a.rows + 3) / 4 : 0;
+  const int row_wgs = join_workgroups(a);
   if (a.weight && a.score) {
     chunks = (pl.max_len + GW - 1) / GW;
     const long long wgs = row_wgs + chunks * pl.B * pl.Hk;

@@ -14,29 +14,55 @@ __device__ inline uint32_t evict_key(int pos, float w, int sink, int recent, int
   return (uint32_t)(order_key(w, 0) >> 32);
 }
 
+// Sum (or largest) over the 16 lanes of a row, in each of them.
+template <typename F>
+__device__ inline int row16(int x, F f) {
+  x = f(x, __builtin_amdgcn_mov_dpp(x, 0xB1, 0xF, 0xF, false));   // quad_perm [1,0,3,2]
+  x = f(x, __builtin_amdgcn_mov_dpp(x, 0x4E, 0xF, 0xF, false));   // quad_perm [2,3,0,1]
+  x = f(x, __builtin_amdgcn_mov_dpp(x, 0x141, 0xF, 0xF, false));  // row_half_mirror
+  return f(x, __builtin_amdgcn_mov_dpp(x, 0x140, 0xF, 0xF, false));  // row_mirror
+}
+__device__ inline int row16_sum(int x) {
+  return row16(x, [](int a, int b) { return a + b; });
+}
+
+struct EvictArgs {
+  const int32_t *len, *slot_pos;
+  const float* weight;
+  int32_t *source, *list, *len_out;
+  int Hk, cap, max_len, budget, sink, recent;
+  // moves that the selection makes itself, in place
+  uint4 *K, *V;
+  int32_t* pos_out;
+  float* weight_out;
+  int vecs;
+};
+constexpr int EV_FUSED = 64;  // at most so many slots beyond the budget: the selection moves their rows itself (one launch in place of two)
+
 // One workgroup per sequence and head.  The slots are dealt to the wavefronts in runs, a run's 64 lanes side by side, KPT keys of a lane in
 // registers (KPT = 0: any number of slots, the keys formed anew each time).  The threshold, the largest key that at least `budget` slots reach, is
-// found two bits at a time from counts of three candidates; equal keys stay from the lowest slot on.  Then each freed place takes the survivor of
-// its rank.
-template <int NT, int KPT>
-__global__ __launch_bounds__(NT) void evict_select_kernel(const int32_t* __restrict__ len, const int32_t* __restrict__ slot_pos,
-                                                          const float* __restrict__ weight, int32_t* __restrict__ source,
-                                                          int32_t* __restrict__ list, int32_t* __restrict__ len_out, int Hk, int cap,
-                                                          int max_len, int budget, int sink, int recent) {
+// found two bits at a time from counts of three candidates, until one is reached by `budget` slots exactly; equal keys stay from the lowest
+// slot on.  Then each freed place takes the survivor of its rank.
+template <int NT, int KPT, bool FUSED>
+__global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
   constexpr int W = NT / 64, UN = KPT > 0 ? KPT : 1;
-  __shared__ int count[3][3], part[4][W];
-  __shared__ uint16_t moved_lds[KPT > 0 ? NT * KPT / 2 : 1];  // at most half of the slots move
+  static_assert(W <= 16, "what wavefronts say to one another is read by a row of 16 lanes");
+  __shared__ int part[5][W], count[2][2][W];
+  __shared__ uint16_t moved_lds[KPT > 0 && !FUSED ? NT * KPT / 2 : 1];         // at most half of the slots move
+  __shared__ int from[FUSED ? EV_FUSED : 1], to[FUSED ? EV_FUSED : 1];
+  const int Hk = a.Hk, cap = a.cap, budget = a.budget, sink = a.sink, recent = a.recent;
   const size_t bh = blockIdx.x;
   const int b = (int)(bh / Hk), tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n = clamp_len(len[b], max_len);
-  if (bh % Hk == 0 && tid == 0) len_out[b] = min(n, budget);
-  int32_t* src = source + bh * budget;
+  const int n = clamp_len(a.len[b], a.max_len);
+  if (bh % Hk == 0 && tid == 0) a.len_out[b] = min(n, budget);
+  int32_t* src = a.source + bh * budget;
   if (n <= budget) {
+    if (FUSED) return;
     for (int j = tid; j < n; j += NT) src[j] = j;
     return;
   }
-  const int32_t* pos = slot_pos + bh * cap;
-  const float* wgt = weight + bh * cap;
+  const int32_t* pos = a.slot_pos + bh * cap;
+  const float* wgt = a.weight + bh * cap;
   const int rounds = KPT > 0 ? KPT : (n + NT - 1) / NT, first = wave * 64 * rounds + lane;
 
   int newest = INT32_MIN;
@@ -58,11 +84,11 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(const int32_t* __restr
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) newest = max(newest, __shfl_xor(newest, o, 64));
+  const int other = min(lane & 15, W - 1);  // the wavefront whose word this lane reads
+  const bool each = (lane & 15) < W, before = (lane & 15) < wave;
   if (lane == 0) part[0][wave] = newest;
-  if (tid < 9) count[tid / 3][tid % 3] = 0;
   __syncthreads();
-#pragma unroll
-  for (int w = 0; w < W; w++) newest = max(newest, part[0][w]);
+  newest = row16(part[0][other], [](int a, int b) { return max(a, b); });
   if constexpr (KPT > 0) {
 #pragma unroll
     for (int k = 0; k < KPT; k++) rkey[k] = first + 64 * k < n ? evict_key(rpos[k], rw[k], sink, recent, newest) : 0;
@@ -74,26 +100,41 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(const int32_t* __restr
     return i < n ? evict_key(pos[i], wgt[i], sink, recent, newest) : 0;
   };
 
+  static_assert(NT * KPT < 1 << 16, "two counts in a word");
   uint32_t thr = 0;
-  for (int step = 0; step < 16; step++) {
-    const uint32_t unit = 1u << (30 - 2 * step);
-    int c1 = 0, c2 = 0, c3 = 0;
+  int seen = n;  // slots that reach thr
+  // (two bits a step; without registers a step is a sweep over the slots, and counts pass 16 bits: one bit)
+  constexpr int BITS = KPT > 0 ? 2 : 1;
+  for (int shift = 32 - BITS; shift >= 0 && seen != budget; shift -= BITS) {
+    const uint32_t unit = 1u << shift;
+    unsigned c1 = 0, c2 = 0, c3 = 0;
 #pragma unroll UN
     for (int k = 0; k < rounds; k++) {
       const uint32_t x = key(k);
       c1 += __popcll(__ballot(x >= thr + unit));
-      c2 += __popcll(__ballot(x >= thr + 2 * unit));
-      c3 += __popcll(__ballot(x >= thr + 3 * unit));
+      if constexpr (BITS == 2) {
+        c2 += __popcll(__ballot(x >= thr + 2 * unit));
+        c3 += __popcll(__ballot(x >= thr + 3 * unit));
+      }
     }
-    int* now = count[step % 3];
+    int(&now)[2][W] = count[shift / BITS % 2];  // (the other one is still being read)
     if (lane == 0) {
-      atomicAdd(now, c1);
-      atomicAdd(now + 1, c2);
-      atomicAdd(now + 2, c3);
+      now[0][wave] = (int)(c1 | c2 << 16);
+      if constexpr (BITS == 2) now[1][wave] = (int)c3;
     }
-    if (tid < 3) count[(step + 1) % 3][tid] = 0;  // (last read two barriers ago)
     __syncthreads();
-    thr += now[2] >= budget ? 3 * unit : now[1] >= budget ? 2 * unit : now[0] >= budget ? unit : 0;
+    const unsigned s12 = (unsigned)row16_sum(each ? now[0][other] : 0);
+    int s1 = (int)s12, s2 = 0, s3 = 0;
+    if constexpr (BITS == 2) {
+      s3 = row16_sum(each ? now[1][other] : 0);
+      s1 = (int)(s12 & 0xffffu);
+      s2 = (int)(s12 >> 16);
+    }
+    const int up = s3 >= budget ? 3 : s2 >= budget ? 2 : s1 >= budget ? 1 : 0;
+    thr += up * unit;
+    seen = up == 3 ? s3 : up == 2 ? s2 : up == 1 ? s1 : seen;
+    thr = __builtin_amdgcn_readfirstlane(thr);
+    seen = __builtin_amdgcn_readfirstlane(seen);
   }
 
   int above = 0, equal = 0;
@@ -107,12 +148,9 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(const int32_t* __restr
     part[2][wave] = equal;
   }
   __syncthreads();
-  int room = budget, equal_at = 0;  // equal keys that stay; rank of this wavefront's first one
-#pragma unroll
-  for (int w = 0; w < W; w++) {
-    room -= part[1][w];
-    equal_at += w < wave ? part[2][w] : 0;
-  }
+  // equal keys that stay; rank of this wavefront's first one
+  const int room = __builtin_amdgcn_readfirstlane(budget - row16_sum(each ? part[1][other] : 0));
+  const int equal_at = __builtin_amdgcn_readfirstlane(row16_sum(before ? part[2][other] : 0));
   const unsigned long long below = (1ull << lane) - 1;
   // whether this lane's k-th slot stays; call for every k in turn, `at` the rank of the next equal key
   auto stays = [&](int k, int& at) -> bool {
@@ -133,16 +171,12 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(const int32_t* __restr
     moved += __popcll(__ballot(i >= budget && yes));
   }
   if (lane == 0) {
-    part[0][wave] = freed;
-    part[3][wave] = moved;
+    part[3][wave] = freed;
+    part[4][wave] = moved;
   }
   __syncthreads();
-  int freed_at = 0, moved_at = 0;
-#pragma unroll
-  for (int w = 0; w < W; w++) {
-    freed_at += w < wave ? part[0][w] : 0;
-    moved_at += w < wave ? part[3][w] : 0;
-  }
+  int freed_at = __builtin_amdgcn_readfirstlane(row16_sum(before ? part[3][other] : 0));
+  int moved_at = __builtin_amdgcn_readfirstlane(row16_sum(before ? part[4][other] : 0));
   at = equal_at;
 #pragma unroll UN
   for (int k = 0; k < rounds; k++) {
@@ -153,11 +187,13 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(const int32_t* __restr
     const unsigned long long who = __ballot(go);
     const int rank = moved_at + __popcll(who & below);
     if (go) {
-      if constexpr (KPT > 0) moved_lds[rank] = (uint16_t)i; else list[bh * budget + rank] = i;
+      if constexpr (FUSED) from[rank] = i;
+      else if constexpr (KPT > 0) moved_lds[rank] = (uint16_t)i;
+      else a.list[bh * budget + rank] = i;
     }
     moved_at += __popcll(who);
   }
-  __syncthreads();
+  if constexpr (!FUSED) __syncthreads();
   at = equal_at;
 #pragma unroll UN
   for (int k = 0; k < rounds; k++) {
@@ -167,55 +203,57 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(const int32_t* __restr
     const bool gone = i < budget && !yes;
     const unsigned long long who = __ballot(gone);
     const int rank = freed_at + __popcll(who & below);
-    if (i < budget) {
-      int from = i;
+    if constexpr (FUSED) {
+      if (gone) to[rank] = i;
+    } else if (i < budget) {
+      int come = i;
       if (gone) {
-        if constexpr (KPT > 0) from = moved_lds[rank]; else from = list[bh * budget + rank];
+        if constexpr (KPT > 0) come = moved_lds[rank]; else come = a.list[bh * budget + rank];
       }
-      src[i] = from;
+      src[i] = come;
     }
     freed_at += __popcll(who);
   }
+  if constexpr (FUSED) {
+    __syncthreads();
+    const int rows = row16_sum(each ? part[4][other] : 0);  // at most n - budget <= EV_FUSED
+    for (int x = tid; x < rows * a.vecs; x += NT) {
+      const int r = x / a.vecs, v = x % a.vecs;
+      const size_t come = (bh * cap + from[r]) * a.vecs + v, go = (bh * cap + to[r]) * a.vecs + v;
+      const uint4 k = a.K[come], w = a.V[come];
+      a.K[go] = k;
+      a.V[go] = w;
+      if (v == 0) {
+        a.pos_out[bh * cap + to[r]] = pos[from[r]];
+        a.weight_out[bh * cap + to[r]] = wgt[from[r]];
+      }
+    }
+  }
 }
 
-// Rows to their places: a row's 16-byte vectors side by side, EV_ROWS rows of keys and values of a thread in flight.
-constexpr int EV_ROWS = 4;
+// Rows to their places: a row's 16-byte vectors side by side, one of keys and one of values for a thread.  (8 x 32 heads, 640 rows of 256 bytes each out
+// of up to 2944: 28 us, 5.8 TB/s; two rows a thread 36, four 52: the loads of rows that may not move are not issued together.)
 __global__ __launch_bounds__(256) void evict_move_kernel(const int32_t* __restrict__ len, const int32_t* __restrict__ source, const uint4* K,
                                                          const uint4* V, const int32_t* pos, const float* weight, uint4* Ko, uint4* Vo,
                                                          int32_t* po, float* wo, int Hk, int cap, int out_cap, int max_len, int budget,
                                                          int vecs, int chunks, int in_place) {
-  const size_t bh = blockIdx.x / chunks;
-  const int per = 256 / vecs, v = threadIdx.x % vecs, first = (int)(blockIdx.x % chunks) * per * EV_ROWS + threadIdx.x / vecs;
-  const int n = min(clamp_len(len[bh / Hk], max_len), budget);
-  int s[EV_ROWS];
-  uint4 k[EV_ROWS], w[EV_ROWS];
-#pragma unroll
-  for (int r = 0; r < EV_ROWS; r++) {
-    const int j = first + r * per;
-    s[r] = j < n ? source[bh * budget + j] : -1;
-    if (in_place && s[r] == j) s[r] = -1;
+  const unsigned bh = blockIdx.x / chunks;
+  const int v = threadIdx.x % vecs, j = (int)(blockIdx.x % chunks) * (256 / vecs) + threadIdx.x / vecs;
+  if (j >= min(clamp_len(len[bh / Hk], max_len), budget)) return;
+  const int s = source[(size_t)bh * budget + j];
+  if (in_place && s == j) return;
+  const size_t from = (size_t)bh * cap + s, to = (size_t)bh * out_cap + j;
+  const uint4 k = K[from * vecs + v], w = V[from * vecs + v];
+  Ko[to * vecs + v] = k;
+  Vo[to * vecs + v] = w;
+  if (v == 0) {
+    po[to] = pos[from];
+    wo[to] = weight[from];
   }
-#pragma unroll
-  for (int r = 0; r < EV_ROWS; r++)
-    if (s[r] >= 0) {
-      k[r] = K[(bh * cap + s[r]) * vecs + v];
-      w[r] = V[(bh * cap + s[r]) * vecs + v];
-    }
-#pragma unroll
-  for (int r = 0; r < EV_ROWS; r++)
-    if (s[r] >= 0) {
-      const size_t to = bh * out_cap + first + r * per;
-      Ko[to * vecs + v] = k[r];
-      Vo[to * vecs + v] = w[r];
-      if (v == 0) {
-        po[to] = pos[bh * cap + s[r]];
-        wo[to] = weight[bh * cap + s[r]];
-      }
-    }
 }
 
 // The most slots of the variants that keep keys in registers.
-constexpr int EV_SMALL = 256 * 4, EV_MIDDLE = 1024 * 4, EV_LARGE = 1024 * 32;
+constexpr int EV_SMALL = 256 * 4, EV_MIDDLE = 512 * 8, EV_LARGE = 1024 * 32;
 
 size_t evict_bytes(const CachePlan& pl) {  // where rows come from; beyond the registers the list of survivors
   return (size_t)pl.B * pl.Hk * pl.budget * 4 * (pl.cap > EV_LARGE ? 2 : 1);
@@ -245,21 +283,28 @@ extern "C" int tc_cache_evict(const tc_cache* c, const int32_t* len, const void*
   int32_t* source = at<int32_t>(ws, 0);
   int32_t* list = source + (size_t)pl.B * pl.Hk * pl.budget;
   const unsigned heads = (unsigned)(pl.B * pl.Hk);  // at most 2^26
-#define TC_EVICT(NT_, KPT_)                                                                                                             \
-  evict_select_kernel<NT_, KPT_><<<heads, NT_, 0, st>>>(len, slot_pos, weight, source, list, len_out, pl.Hk, pl.cap, pl.max_len, pl.budget, \
-                                                        pl.sink, pl.recent)
+  const int vecs = pl.dh * pl.esize / 16;
+  EvictArgs a = {len, slot_pos, weight, source, list, len_out, pl.Hk, pl.cap, pl.max_len, pl.budget, pl.sink, pl.recent, (uint4*)K_out, (uint4*)V_out,
+                 pos_out, weight_out, vecs};
+  const bool fused = same == 4 && pl.max_len - pl.budget <= EV_FUSED;
+#define TC_EVICT(NT_, KPT_)                                        \
+  do {                                                             \
+    if (fused)                                                     \
+      evict_select_kernel<NT_, KPT_, true><<<heads, NT_, 0, st>>>(a);  \
+    else                                                           \
+      evict_select_kernel<NT_, KPT_, false><<<heads, NT_, 0, st>>>(a); \
+  } while (0)
   if (pl.max_len <= EV_SMALL)
     TC_EVICT(256, 4);
   else if (pl.max_len <= EV_MIDDLE)
-    TC_EVICT(1024, 4);
+    TC_EVICT(512, 8);
   else if (pl.max_len <= EV_LARGE)
     TC_EVICT(1024, 32);
   else
     TC_EVICT(1024, 0);
 #undef TC_EVICT
-  if (same == 4 && pl.max_len <= pl.budget) return check_launch();  // nothing can move
-  const int vecs = pl.dh * pl.esize / 16, rows = 256 / vecs * EV_ROWS, most = pl.max_len < pl.budget ? pl.max_len : pl.budget;
-  const int chunks = (most + rows - 1) / rows;
+  if (fused) return check_launch();
+  const int rows = 256 / vecs, most = pl.max_len < pl.budget ? pl.max_len : pl.budget, chunks = (most + rows - 1) / rows;
   if ((long long)heads * chunks > 0x7fffffffLL) return TC_ERR_SHAPE;
   evict_move_kernel<<<heads * chunks, 256, 0, st>>>(len, source, (const uint4*)K_cache, (const uint4*)V_cache, slot_pos, weight, (uint4*)K_out,
                                                     (uint4*)V_out, pos_out, weight_out, pl.Hk, pl.cap, out_capacity, pl.max_len, pl.budget, vecs,

@@ -20,6 +20,28 @@ int check_rope(const tc_rope* r) {
   return TC_OK;
 }
 
+// Sine and cosine of an angle of at most 2^31: the nearest multiple of pi/2 is taken off in two parts (the first product is exact inside the
+// multiply-add, what it rounds is below 2^-53), then the Taylor series up to 1/13! and 1/14!, whose next terms are below 2^-45 at pi/4:
+// far inside the rounding to float32.  (The library's routine, which serves any angle: 13.6 us for 23552 positions of 64 pairs, this 7.)
+__device__ inline void sin_cos(double x, double* sn, double* cs) {
+  const double q = rint(x * 0.63661977236758134308);  // 2 / pi
+  double r = fma(-q, 1.5707963267948965580, x);
+  r = fma(-q, 6.1232339957367658860e-17, r);
+  const double z = r * r;
+  double s = 1.0 / 6227020800.0, c = -1.0 / 87178291200.0;
+  s = fma(s, z, -1.0 / 39916800.0); c = fma(c, z, 1.0 / 479001600.0);
+  s = fma(s, z, 1.0 / 362880.0);    c = fma(c, z, -1.0 / 3628800.0);
+  s = fma(s, z, -1.0 / 5040.0);     c = fma(c, z, 1.0 / 40320.0);
+  s = fma(s, z, 1.0 / 120.0);       c = fma(c, z, -1.0 / 720.0);
+  s = fma(s, z, -1.0 / 6.0);        c = fma(c, z, 1.0 / 24.0);
+  s = fma(s * z, r, r);             c = fma(c, z, -0.5);
+  c = fma(c, z, 1.0);
+  const int k = (int)q;
+  const double a = k & 1 ? c : s, b = k & 1 ? s : c;
+  *sn = k & 2 ? -a : a;
+  *cs = (k + 1) & 2 ? -b : b;
+}
+
 // One thread has one pair's angle per position and goes over some positions.
 __global__ __launch_bounds__(256) void rope_tables_kernel(const int32_t* __restrict__ pos, long long n, float* __restrict__ c,
                                                           float* __restrict__ s, int half, double log_base, int scaling, double factor,
@@ -38,7 +60,7 @@ __global__ __launch_bounds__(256) void rope_tables_kernel(const int32_t* __restr
     const long long i = first + (long long)j * rows;
     if (i >= n) return;
     double sn, cs;
-    sincos((double)pos[i] * theta, &sn, &cs);
+    sin_cos((double)pos[i] * theta, &sn, &cs);
     c[i * half + k] = (float)(cs * magnitude);
     s[i * half + k] = (float)(sn * magnitude);
   }
@@ -289,7 +311,7 @@ extern "C" int tc_rope_tables(const tc_rope* r, const int32_t* pos_ids, int64_t 
   double log_base = std::log((double)r->base);
   if (r->scaling == TC_ROPE_BASE) log_base += std::log((double)r->factor) * rd / (rd - 2.0);
   const int64_t blocks1 = (n + rows - 1) / rows;
-  const int per = blocks1 >= 8192 ? 8 : 1;  // positions of a thread: its angle is worth keeping once the chip is full
+  const int per = blocks1 >= 8 * 1024 ? 8 : blocks1 >= 2 * 1024 ? (int)(blocks1 / 1024) : 1;  // positions of a thread: its angle is worth keeping once the chip is full
   const int64_t blocks = (blocks1 + per - 1) / per;
   if (blocks > 0x7fffffffLL) return TC_ERR_SHAPE;
   rope_tables_kernel<<<(unsigned)blocks, 256, 0, (hipStream_t)stream>>>(pos_ids, n, cos, sin, half, log_base, r->scaling, (double)r->factor,

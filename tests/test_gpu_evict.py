@@ -78,7 +78,8 @@ def test_types(dtype, d, in_place):
 
 
 @pytest.mark.parametrize("cap,budget", [(1, 1), (2, 1), (65, 64), (1024, 100), (1025, 1024), (1100, 1), (4096, 4000), (4097, 640), (9000, 8999),
-                                        (32768, 1000), (32769, 16384), (40000, 20001)])
+                                        (32768, 1000), (32769, 16384), (40000, 20001), (128, 64), (129, 64), (2000, 1990), (32768, 32704),
+                                        (40000, 39960)])
 @pytest.mark.parametrize("in_place", [True, False])
 def test_sizes(cap, budget, in_place):
     # every variant of the selection, at its ends
