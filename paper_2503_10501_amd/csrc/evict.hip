@@ -7,11 +7,11 @@
 
 namespace tc {
 
-// A slot's place in the order, larger is better: protected slots first, then weights descending (+0 and -0 alike), NaN last.  Never 0.
-__device__ inline uint32_t evict_key(int pos, float w, int sink, int recent, int newest) {
-  if (pos < sink || (long long)pos > (long long)newest - recent) return 0xffffffffu;
-  if (w != w) w = -INFINITY;
-  return (uint32_t)(order_key(w, 0) >> 32);
+// A slot's place in the order, larger is better: protected slots (position below `sink`, or `late` and above) first, then weights descending
+// (+0 and -0 alike), NaN last.  Never 0.
+__device__ inline uint32_t evict_key(int pos, float w, int sink, bool any_late, int late) {
+  const uint32_t key = (uint32_t)(order_key(w == w ? w : -INFINITY, 0) >> 32);
+  return pos < sink || (any_late && pos >= late) ? 0xffffffffu : key;
 }
 
 // Sum (or largest) over the 16 lanes of a row, in each of them.
@@ -73,8 +73,8 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
 #pragma unroll
     for (int k = 0; k < KPT; k++) {
       const int i = first + 64 * k;
-      rpos[k] = i < n ? pos[i] : INT32_MIN;
-      rw[k] = i < n ? wgt[i] : 0.f;
+      rpos[k] = pos[min(i, n - 1)];  // (behind the last slot that one again)
+      rw[k] = wgt[min(i, n - 1)];
     }
 #pragma unroll
     for (int k = 0; k < KPT; k++) newest = max(newest, rpos[k]);
@@ -89,15 +89,18 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
   if (lane == 0) part[0][wave] = newest;
   __syncthreads();
   newest = row16(part[0][other], [](int a, int b) { return max(a, b); });
+  const long long from_late = (long long)newest - recent + 1;
+  const int late = from_late < INT32_MIN ? INT32_MIN : (int)from_late;
+  const bool any_late = recent > 0;
   if constexpr (KPT > 0) {
 #pragma unroll
-    for (int k = 0; k < KPT; k++) rkey[k] = first + 64 * k < n ? evict_key(rpos[k], rw[k], sink, recent, newest) : 0;
+    for (int k = 0; k < KPT; k++) rkey[k] = first + 64 * k < n ? evict_key(rpos[k], rw[k], sink, any_late, late) : 0;
   }
   // key of this lane's k-th slot, 0 behind the last one
   auto key = [&](int k) -> uint32_t {
     if constexpr (KPT > 0) return rkey[k];
     const int i = first + 64 * k;
-    return i < n ? evict_key(pos[i], wgt[i], sink, recent, newest) : 0;
+    return i < n ? evict_key(pos[i], wgt[i], sink, any_late, late) : 0;
   };
 
   static_assert(NT * KPT < 1 << 16, "two counts in a word");
