@@ -123,6 +123,7 @@ struct AttnArgs {
 struct Job {
   int groups, rows, tiles, splits, part0;  // part0: the first of the `splits` parts that this share writes
   bool packed, prefix, cache, many;        // many: by many_kernel
+  bool wide;                               // eight wavefronts
 };
 
 // Row r of a group: its place among all rows.
@@ -201,7 +202,25 @@ __device__ __forceinline__ void zero_behind(int there, int id, u4 (&vr)[NV]) {
     if (id + N * j >= there * VEC) vr[j] = u4{0, 0, 0, 0};
 }
 
-// ---- few rows: one workgroup has 16 rows, its four wavefronts share the keys, 32 at a time, without waiting for one another ----
+// Slots k .. k + 3 of a sequence and head gather the probabilities of its few rows, from the scores that were kept.  A row's scores are there up to
+// the tile that the last row sees; behind what the row sees they are not looked at.
+__device__ inline void add_weights(const AttnArgs& a, int group, int k, int n, int m, const float* lse) {
+  float* w = a.weight + (size_t)group * a.cap + k;
+  f4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int r = 0; r < a.R; r++) {
+    const int end = seen(a, r, n, m);
+    f4 s = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    if (k < end && lse[r] < INFINITY) s = *reinterpret_cast<const f4*>(a.score + (size_t)(group * a.R + r) * a.score_ld + k);
+#pragma unroll
+    for (int e = 0; e < 4; e++) acc[e] += k + e < end && lse[r] < INFINITY ? exp2_fast(s[e] - lse[r]) : 0.f;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; e++)
+    if (k + e < n) w[e] += acc[e];
+}
+
+// ---- few rows: one workgroup has 16 rows, its four or eight wavefronts share the keys, 32 at a time, without waiting for one another ----
 
 constexpr int FK = 32;  // keys of a wavefront's tile
 template <typename T, int DH>
@@ -209,20 +228,21 @@ struct FewShape {
   static constexpr int ES = sizeof(T), VEC = DH * ES / 16;             // 16-byte vectors of a row
   static constexpr int KLD = DH * ES + 16, VLD = DH * ES + (ES == 2 ? 32 : 16);  // rows in LDS: lanes of a product's operand meet other banks
   static constexpr int NV = FK * VEC / 64;                             // vectors of a lane
-  static constexpr int WAVE = FK * (KLD + VLD), LDS = 4 * WAVE;
+  static constexpr int WAVE = FK * (KLD + VLD);
+  static constexpr int MOST = 8 * WAVE <= 160 * 1024 - 2048 ? 8 : 4;   // wavefronts that fit
   static_assert(16 * (DH + 4) * 4 <= WAVE, "the partial output takes the place of the tiles");
 };
 
 // KEEP: scores of the cache's keys are written.  Unconditionally, so that the count of accesses in flight is known and a tile's loads need not wait
 // for them: lanes behind the last row have its scores, and scores of a prefix go to FK places behind a row's own.
-template <typename T, int DH, bool KEEP>
-__global__ __launch_bounds__(256) void few_kernel(AttnArgs a, Job first, Job second) {
+template <typename T, int DH, bool KEEP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void few_kernel(AttnArgs a, Job first, Job second) {
   typedef FewShape<T, DH> S;
   typedef Mma<T> M;
   typedef typename M::frag frag;
   constexpr int ES = S::ES, VEC = S::VEC, NV = S::NV, DT = DH / 16;
   extern __shared__ __attribute__((aligned(16))) unsigned char cache_smem[];
-  __shared__ float wave_m[4][16], wave_l[4][16], row_sum[16];  // row_sum: infinite for a row whose output is zero
+  __shared__ float wave_m[WAVES][16], wave_l[WAVES][16], row_sum[16], row_lse[16];  // row_sum: infinite for a row whose output is zero
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
   const unsigned in_first = (unsigned)first.groups * first.tiles * first.splits;
   const bool other = blockIdx.x >= in_first;
@@ -275,7 +295,7 @@ __global__ __launch_bounds__(256) void few_kernel(AttnArgs a, Job first, Job sec
 
   int t = t0 + wave;
   if (t < t1) fetch(t);
-  for (; t < t1; t += 4) {
+  for (; t < t1; t += WAVES) {
     const bool pre = t < np;
     const int k0 = (pre ? t : t - np) * FK, last = pre ? a.P : most;
     const bool masked = k0 + FK > (pre ? a.P : least);  // some row does not see some key
@@ -296,7 +316,7 @@ __global__ __launch_bounds__(256) void few_kernel(AttnArgs a, Job first, Job sec
       *reinterpret_cast<u4*>(Ks + key * S::KLD + c * 16) = kr[j];
       *reinterpret_cast<u4*>(Vs + key * S::VLD + c * 16) = vr[j];
     }
-    if (t + 4 < t1) fetch(t + 4);
+    if (t + WAVES < t1) fetch(t + WAVES);
     wave_lds_order();
 
     f4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
@@ -381,7 +401,7 @@ __global__ __launch_bounds__(256) void few_kernel(AttnArgs a, Job first, Job sec
   }
   sum = col_sum(sum);
 
-  // the four wavefronts' parts
+  // the wavefronts' parts
   if (g == 0) {
     wave_m[wave][i] = mx;
     wave_l[wave][i] = sum;
@@ -389,27 +409,29 @@ __global__ __launch_bounds__(256) void few_kernel(AttnArgs a, Job first, Job sec
   __syncthreads();
   float top = -INFINITY, total = 0.f;
 #pragma unroll
-  for (int w = 0; w < 4; w++) top = fmaxf(top, wave_m[w][i]);
+  for (int w = 0; w < WAVES; w++) top = fmaxf(top, wave_m[w][i]);
   const float ref = top == -INFINITY ? 0.f : top;
 #pragma unroll
-  for (int w = 0; w < 4; w++) total += wave_l[w][i] * exp2_fast(wave_m[w][i] - ref);
+  for (int w = 0; w < WAVES; w++) total += wave_l[w][i] * exp2_fast(wave_m[w][i] - ref);
   const float f = exp2_fast(mx - ref);
   float* part = reinterpret_cast<float*>(cache_smem + wave * S::WAVE);
 #pragma unroll
   for (int d = 0; d < DT; d++) *reinterpret_cast<f4*>(part + i * (DH + 4) + 16 * d + 4 * g) = o[d] * f;
   if (threadIdx.x < 16 && mine) {  // (wavefront 0, lane i: row i)
+    const float lse = live ? ref + a.offset + log2f(total) : INFINITY;
     if (a.parts > 1) a.ml[(size_t)(job.part0 + split) * a.rows + row] = f2{top == -INFINITY ? top : top + a.offset, total};
-    else if (a.lse) a.lse[row] = live ? ref + a.offset + log2f(total) : INFINITY;
+    else if (a.lse) a.lse[row] = lse;
+    row_lse[i] = lse;
     row_sum[i] = live && a.P + end > 0 ? total : INFINITY;
   }
   __syncthreads();
   if (a.parts > 1 && t0 >= t1) return;
-  for (int at = threadIdx.x; at < 16 * DH / 4; at += 256) {
+  for (int at = threadIdx.x; at < 16 * DH / 4; at += 64 * WAVES) {
     const int rr = at / (DH / 4), c = at % (DH / 4);
     if (tile * 16 + rr >= job.rows) continue;
     f4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < 4; w++) v += *reinterpret_cast<const f4*>(cache_smem + w * S::WAVE + (rr * (DH + 4) + 4 * c) * 4);
+    for (int w = 0; w < WAVES; w++) v += *reinterpret_cast<const f4*>(cache_smem + w * S::WAVE + (rr * (DH + 4) + 4 * c) * 4);
     const int to = row_of(a, job, group, tile * 16 + rr);
     if (a.parts > 1) {
       *reinterpret_cast<f4*>(a.part + ((size_t)(job.part0 + split) * a.rows + to) * DH + 4 * c) = v;
@@ -420,9 +442,13 @@ __global__ __launch_bounds__(256) void few_kernel(AttnArgs a, Job first, Job sec
       for (int e = 0; e < 4; e++) out[e] = Vec16<T>::round(v[e]);
     }
   }
+  // the only part: this workgroup has written all scores of its rows (and the barriers above stand between)
+  if (KEEP && a.parts == 1)
+    for (int k = 4 * threadIdx.x; k < n; k += 4 * 64 * WAVES) add_weights(a, group, k, n, m, row_lse);
 }
 
-// ---- many rows, 16-bit storage: one workgroup has 128 rows, a wavefront 32 of them, all go over the same tiles of 64 keys ----
+// ---- many rows, 16-bit storage: one workgroup has 128 rows, a wavefront 32 of them, all go over the same tiles of 64 keys; or (KW = 2) 64 rows,
+// and two wavefronts share the keys of a tile ----
 //
 // Products of 32 x 32 tiles: a lane has row lane % 32, and of each 32 keys those with (key / 4) % 2 = lane / 32, which are the ones that its
 // operand of the second product wants.  A tile is in one of two stages of LDS while the next one is written into the other and the one
@@ -433,14 +459,15 @@ struct ManyShape {
   static constexpr int VEC = DH / 8, NV = MK * VEC / 256;         // 16-byte vectors of a row, of a thread
   static constexpr int KLD = DH * 2 + 16, VLD = DH * 2 + 64;      // rows in LDS: 16 lanes of a read meet other banks
   static constexpr int STAGE = MK * (KLD + VLD), LDS = 2 * STAGE;
-  static_assert(4 * 32 * KLD <= LDS, "the output takes the place of the tiles");
+  static_assert(4 * 32 * KLD <= LDS && 2 * 64 * (DH / 2 + 2) * 4 + 2 * 32 * KLD <= LDS, "outputs take the place of the tiles");
 };
 // The running maximum is raised when a row's passes it by more than 2^8: up to there the probabilities are larger than 1, which neither
 // the sums in float32 nor the heads mind, and the partial output need not be scaled.
 constexpr float LAZY = 8.f;
 
-template <typename T, int DH>
+template <typename T, int DH, int KW>
 struct ManyWave {
+  static constexpr int NU = 2 / KW;  // runs of 32 keys of a tile that are the wavefront's
   typedef Mma<T> M;
   typedef typename M::frag frag;
   typedef ManyShape<DH> S;
@@ -453,28 +480,30 @@ struct ManyWave {
   __device__ __forceinline__ void step(const unsigned char* Ks, const unsigned char* Vs, int k0, int lim, bool masked, float scale2, float offset,
                                        int lane) {
     const int half = lane >> 5, i = lane & 31;
-    f16v s[2];
+    f16v s[NU];
 #pragma unroll
-    for (int e = 0; e < 16; e++) s[0][e] = s[1][e] = 0.f;
+    for (int u = 0; u < NU; u++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) s[u][e] = 0.f;
     const unsigned char* kr = Ks + i * S::KLD + 16 * half;
 #pragma unroll
     for (int c = 0; c < DH / 16; c++)
 #pragma unroll
-      for (int u = 0; u < 2; u++) {
+      for (int u = 0; u < NU; u++) {
         frag k;
         k.u = *reinterpret_cast<const u4*>(kr + u * 32 * S::KLD + 32 * c);
         s[u] = M::mul32(k, q[c], s[u]);
       }
     if (masked) {
 #pragma unroll
-      for (int u = 0; u < 2; u++)
+      for (int u = 0; u < NU; u++)
 #pragma unroll
         for (int e = 0; e < 16; e++)
           if (k0 + 32 * u + 8 * (e >> 2) + 4 * half + (e & 3) >= lim) s[u][e] = -INFINITY;
     }
     float top = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < 2; u++)
+    for (int u = 0; u < NU; u++)
 #pragma unroll
       for (int e = 0; e < 16; e++) top = fmaxf(top, s[u][e]);
     const u2 w = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
@@ -488,7 +517,7 @@ struct ManyWave {
     }
     const float ref = mx == -INFINITY ? 0.f : mx + offset;
 #pragma unroll
-    for (int u = 0; u < 2; u++) {
+    for (int u = 0; u < NU; u++) {
       float p[16];
 #pragma unroll
       for (int e = 0; e < 16; e++) {
@@ -530,10 +559,11 @@ struct ManyWave {
   }
 };
 
-template <typename T, int DH>
+template <typename T, int DH, int KW>
 __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
   typedef ManyShape<DH> S;
-  typedef ManyWave<T, DH> Wave;
+  typedef ManyWave<T, DH, KW> Wave;
+  constexpr int ROWS = MROWS / KW, RW = 4 / KW;  // rows of the workgroup, wavefronts that share them
   extern __shared__ __attribute__((aligned(16))) unsigned char cache_smem[];
   __shared__ int ends[2][4], flag[3];
   __shared__ size_t places[4][32];  // of rows in the output
@@ -542,15 +572,17 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
   const int split = item % job.splits, tile = job.tiles - 1 - item / job.splits;  // (the rows that see the most first)
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, i = lane & 31;
   const int hk = group % a.Hk, b = group / a.Hk;  // (packed: b is the image)
-  const int r = tile * MROWS + wave * 32 + i, row = row_of(a, job, group, min(r, job.rows - 1));
-  const bool mine = r < job.rows, idle = tile * MROWS + wave * 32 >= job.rows;
+  // The tiles are laid so that the last one is full: the empty rows are in the first one, which sees the fewest keys.
+  const int r0 = tile * ROWS - (job.tiles * ROWS - job.rows) + wave % RW * 32, r = r0 + i, row = row_of(a, job, group, max(r, 0));
+  const int ku = KW == 2 ? wave / RW * 32 : 0;  // the wavefront's first key of a tile
+  const bool mine = r >= 0, idle = r0 + 31 < 0;
   int m = 1, end = 0;
   bool live = mine;
   if (job.cache) {
     const int n = clamp_len(a.len[b], a.max_len);
     m = a.q_len ? clamp_len(a.q_len[b], a.T) : a.T;
     live = mine && r % a.T < m;
-    end = m > 0 ? seen(a, min(r, a.R - 1), n, m) : 0;
+    end = m > 0 ? seen(a, max(r, 0), n, m) : 0;
   }
   int most = end, least = end;
 #pragma unroll
@@ -621,13 +653,13 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
   }
   for (int t = t0; t < t1; t++) {
     const bool pre = t < np;
-    const int k0 = (pre ? t : t - np) * MK, lim = pre ? a.P : end;
+    const int k0 = (pre ? t : t - np) * MK + ku, lim = pre ? a.P : end;
     const unsigned char* Ks = cache_smem + (t & 1) * S::STAGE;
-    if (!idle && (pre || k0 < wave_most)) {
-      const bool masked = k0 + MK > (pre ? a.P : wave_least);
-      w.step(Ks, Ks + MK * S::KLD, k0, lim, masked, a.scale2, a.offset, lane);
+    if (!idle && k0 < (pre ? a.P : wave_most)) {
+      const bool masked = k0 + MK / KW > (pre ? a.P : wave_least);
+      w.step(Ks + ku * S::KLD, Ks + MK * S::KLD + ku * S::VLD, k0, lim, masked, a.scale2, a.offset, lane);
       if (masked && __builtin_amdgcn_readfirstlane(flag[t % 3]))
-        w.add_odd(static_cast<const T*>(pre ? a.Vp : a.Vc) + ((pre ? phead : head) + k0) * DH, min(MK, (pre ? a.P : most) - k0), lim - k0, lane);
+        w.add_odd(static_cast<const T*>(pre ? a.Vp : a.Vc) + ((pre ? phead : head) + k0) * DH, min(MK / KW, (pre ? a.P : most) - k0), lim - k0, lane);
     }
     if (tid == 0) flag[(t + 2) % 3] = 0;  // (last looked at before the last barrier, set again behind the next one)
     if (t + 1 < t1) store(t + 1);         // the other stage was last read before the last barrier
@@ -635,7 +667,29 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
     if (t + 2 < t1) fetch(t + 2);
   }
   const u2 x = __builtin_amdgcn_permlane32_swap(__float_as_uint(w.sum), __float_as_uint(w.sum), false, false);
-  const float total = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+  float total = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+  if constexpr (KW == 2) {  // the second wavefront of the rows hands its share to the first (behind the last barrier nobody reads the tiles)
+    float* at = reinterpret_cast<float*>(cache_smem) + wave % RW * (64 * (DH / 2 + 2)) + lane;
+    if (wave >= RW) {
+      at[0] = w.mx;
+      at[64] = total;
+#pragma unroll
+      for (int d = 0; d < DH / 32; d++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) at[64 * (2 + 16 * d + e)] = w.o[d][e];
+    }
+    __syncthreads();
+    if (wave >= RW) return;
+    const float mx = fmaxf(w.mx, at[0]), ref = mx == -INFINITY ? 0.f : mx;
+    const float f0 = exp2_fast(w.mx - ref), f1 = exp2_fast(at[0] - ref);
+    total = total * f0 + at[64] * f1;
+#pragma unroll
+    for (int d = 0; d < DH / 32; d++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) w.o[d][e] = w.o[d][e] * f0 + at[64 * (2 + 16 * d + e)] * f1;
+    w.mx = mx;
+    wave_lds_order();
+  }
   if (a.parts > 1) {
     if (!mine) return;
     const size_t at = (size_t)(job.part0 + split) * a.rows + row;
@@ -652,7 +706,7 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
   if (a.lse && half == 0 && mine) a.lse[row] = live ? (w.mx == -INFINITY ? 0.f : w.mx) + a.offset + log2f(total) : INFINITY;
   const bool sees = live && a.P + end > 0;
   const float inv = 1.f / total;
-  unsigned char* Os = cache_smem + wave * 32 * S::KLD;  // (behind the last barrier nobody reads the tiles)
+  unsigned char* Os = cache_smem + 2 * 64 * (DH / 2 + 2) * 4 * (KW - 1) + wave * 32 * S::KLD;
   if (half == 0) places[wave][i] = out_row(a, row, DH);
 #pragma unroll
   for (int d = 0; d < DH / 32; d++)
@@ -665,7 +719,7 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
 #pragma unroll
   for (int j = 0; j < 32 * S::VEC / 64; j++) {
     const int at = lane + 64 * j, rr = at / S::VEC, c = at % S::VEC;
-    if (tile * MROWS + wave * 32 + rr < job.rows)
+    if (r0 + rr >= 0)
       *reinterpret_cast<u4*>(static_cast<T*>(a.O) + places[wave][rr] + 8 * c) = *reinterpret_cast<const u4*>(Os + rr * S::KLD + c * 16);
   }
 }
@@ -767,32 +821,12 @@ __global__ __launch_bounds__(256) void join_gather_kernel(AttnArgs a, int row_wg
     float ref, total;
     bool sees;
     const bool live = row_live(a, row, sees);
-    if (a.parts > 1) {
-      row_stats(a, row, lane, ref, total);
-      ref += log2f(total);
-    } else {
-      ref = a.lse[row];
-    }
-    if (lane == 0) lse[r] = live ? ref : INFINITY;
+    row_stats(a, row, lane, ref, total);
+    if (lane == 0) lse[r] = live ? ref + log2f(total) : INFINITY;
   }
   __syncthreads();
   const int k = first + 4 * (int)threadIdx.x;
-  if (k >= n) return;
-  float* w = a.weight + (size_t)bh * a.cap + k;
-  f4 acc = {0.f, 0.f, 0.f, 0.f};
-  const int m = a.q_len ? clamp_len(a.q_len[b], a.T) : a.T;
-#pragma unroll 4
-  for (int r = 0; r < a.R; r++) {
-    // a row's scores are there up to the tile that its group's last row sees; behind what the row sees they are not looked at
-    const int end = seen(a, r, n, m);
-    f4 s = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    if (k < end && lse[r] < INFINITY) s = *reinterpret_cast<const f4*>(a.score + (size_t)(bh * a.R + r) * a.score_ld + k);
-#pragma unroll
-    for (int e = 0; e < 4; e++) acc[e] += k + e < end && lse[r] < INFINITY ? exp2_fast(s[e] - lse[r]) : 0.f;
-  }
-#pragma unroll
-  for (int e = 0; e < 4; e++)
-    if (k + e < n) w[e] += acc[e];
+  if (k < n) add_weights(a, bh, k, n, a.q_len ? clamp_len(a.q_len[b], a.T) : a.T, lse);
 }
 
 // What slots gather: 16 keys per wavefront, kept in registers; the rows of queries pass by, 16 at a time.
@@ -810,6 +844,7 @@ __global__ __launch_bounds__(256) void gather_kernel(AttnArgs a, int chunks) {
 #pragma unroll
   for (int s = 0; s < DH / 32; s++) k[s] = frag_of<T>(Kr, 4 * s + g);
   f4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
   for (int r0 = 0; r0 < a.R; r0 += 16) {
     const int r = min(r0 + i, a.R - 1);
     const size_t row = (size_t)bh * a.R + r;
@@ -835,14 +870,18 @@ __global__ __launch_bounds__(256) void gather_kernel(AttnArgs a, int chunks) {
 // How a call is cut.  The prefix of an image's sequences is read once for all of them where the rows of one sequence do not fill a
 // tile by themselves; else a sequence's rows go over its prefix and its cache in one sweep.
 constexpr int FEW_ROWS = 16;
-static Job make_job(const CachePlan& pl, int groups, int rows, int keys, bool packed, bool prefix, bool cache) {
+static Job make_job(const CachePlan& pl, int groups, int rows, int keys, bool packed, bool prefix, bool cache, bool alone) {
   const bool many = rows > FEW_ROWS && pl.esize == 2;
-  const int per = many ? MROWS : FEW_ROWS, tile = many ? MK : FK, least = many ? 2 : 4;
-  Job j = {groups, rows, (rows + per - 1) / per, 1, 0, packed, prefix, cache, many};
+  const int per = !many ? FEW_ROWS : rows <= MROWS / 2 ? MROWS / 2 : MROWS, tile = many ? MK : FK, least = many ? 2 : 4;
+  Job j = {groups, rows, (rows + per - 1) / per, 1, 0, packed, prefix, cache, many, false};
+  const long long items = (long long)groups * j.tiles, tiles = (keys + tile - 1) / tile + (prefix && cache ? 1 : 0);
+  // Few rows on a part of the chip, up to 768 keys: eight wavefronts take all keys, and nothing has to be joined.  (One sequence, 32 heads,
+  // us in one sweep and in parts: 640 keys 10.5 and 11.9, 1000 14.3 and 12.5, 2000 21 and 15.)
+  j.wide = !many && alone && items <= 256 && tiles > 4 && tiles <= 24 && !(pl.esize == 4 && pl.dh == 128);
+  if (j.wide) return j;
   // Parts of the keys: two workgroups for each compute unit, if there is a tile for each wavefront (many: two for the workgroup).  Few rows
   // of long caches take four of them, which evens out sequences of different lengths, where a wavefront still has four tiles.  (us, two and
   // four: 4 sequences of up to 32768 keys 99 and 94; one 24 and 29; 64 sequences sharing 8 prefixes of 640 keys 52 and 57.)
-  const long long items = (long long)groups * j.tiles, tiles = (keys + tile - 1) / tile + (prefix && cache ? 1 : 0);
   long long s = (512 + items - 1) / items;
   if (s > (tiles + least - 1) / least) s = (tiles + least - 1) / least;
   if (!many) {
@@ -860,15 +899,17 @@ struct Cut {
 };
 static Cut make_cut(const CachePlan& pl, int max_len) {
   Cut c = {};
-  if (pl.images > 0 && pl.each > 1 && pl.R <= FEW_ROWS) {
+  // Reading a prefix once pays for a second kind of parts and their joining (5 us) from 32 MB on that are not read again.
+  const double again = (double)pl.images * (pl.each - 1) * pl.Hk * pl.P * pl.dh * 2.0 * pl.esize;
+  if (pl.images > 0 && pl.R <= FEW_ROWS && again >= 32e6) {
     c.jobs = 2;
-    c.job[0] = make_job(pl, pl.images * pl.Hk, pl.each * pl.R, pl.P, true, true, false);
-    c.job[1] = make_job(pl, pl.B * pl.Hk, pl.R, max_len, false, false, true);
+    c.job[0] = make_job(pl, pl.images * pl.Hk, pl.each * pl.R, pl.P, true, true, false, false);
+    c.job[1] = make_job(pl, pl.B * pl.Hk, pl.R, max_len, false, false, true, false);
     c.job[1].part0 = c.job[0].splits;
     c.parts = c.job[0].splits + c.job[1].splits;
   } else {
     c.jobs = 1;
-    c.job[0] = make_job(pl, pl.B * pl.Hk, pl.R, pl.P + max_len, false, pl.P > 0, true);
+    c.job[0] = make_job(pl, pl.B * pl.Hk, pl.R, pl.P + max_len, false, pl.P > 0, true, true);
     c.parts = c.job[0].splits;
   }
   return c;
@@ -877,8 +918,9 @@ static Cut make_cut(const CachePlan& pl, int max_len) {
 // Rows of parts (none where a row has a single one).
 static size_t part_rows(const CachePlan& pl) {
   if (pl.B == 0) return 0;
-  const Cut c = make_cut(pl, pl.cap);  // (longer caches are cut into no fewer parts)
-  return c.parts > 1 ? (size_t)pl.B * pl.H * pl.T * c.parts : 0;
+  // the most parts of any max_len: longer caches are cut into no fewer
+  const int parts = make_cut(pl, pl.cap).parts;
+  return parts > 1 ? (size_t)pl.B * pl.H * pl.T * parts : 0;
 }
 // Few rows of a sequence: their scores are kept, so that the keys are read once.
 static bool keeps_scores(const CachePlan& pl) { return pl.R <= FEW_ROWS; }
@@ -911,17 +953,22 @@ static int attention_launch(const CachePlan& pl, AttnArgs a, hipStream_t st) {
       continue;
     }
     if constexpr (sizeof(T) == 2) {
-      if (!allow_lds(many_kernel<T, DH>, ManyShape<DH>::LDS)) return TC_ERR_HIP;
-      many_kernel<T, DH><<<(unsigned)workgroups(cut.job[k]), 256, ManyShape<DH>::LDS, st>>>(a, cut.job[k]);
+      const auto kernel = cut.job[k].rows <= MROWS / 2 ? many_kernel<T, DH, 2> : many_kernel<T, DH, 1>;
+      if (!allow_lds(kernel, ManyShape<DH>::LDS)) return TC_ERR_HIP;
+      kernel<<<(unsigned)workgroups(cut.job[k]), 256, ManyShape<DH>::LDS, st>>>(a, cut.job[k]);
     }
   }
   if (nf > 0) {
-    const auto kernel = a.score ? few_kernel<T, DH, true> : few_kernel<T, DH, false>;
-    if (!allow_lds(kernel, FewShape<T, DH>::LDS)) return TC_ERR_HIP;
-    kernel<<<(unsigned)(workgroups(few[0]) + workgroups(few[1])), 256, FewShape<T, DH>::LDS, st>>>(a, few[0], few[1]);
+    typedef FewShape<T, DH> F;
+    const int waves = few[0].wide ? F::MOST : 4;
+    const auto kernel = waves == 8 ? (a.score ? few_kernel<T, DH, true, F::MOST> : few_kernel<T, DH, false, F::MOST>)
+                                   : (a.score ? few_kernel<T, DH, true, 4> : few_kernel<T, DH, false, 4>);
+    if (!allow_lds(kernel, waves * F::WAVE)) return TC_ERR_HIP;
+    kernel<<<(unsigned)(workgroups(few[0]) + workgroups(few[1])), 64 * waves, waves * F::WAVE, st>>>(a, few[0], few[1]);
   }
   const int row_wgs = join_workgroups(a);
   if (a.weight && a.score) {
+    if (a.parts == 1) return check_launch();  // done by few_kernel
     chunks = (pl.max_len + GW - 1) / GW;
     const long long wgs = row_wgs + chunks * pl.B * pl.Hk;
     if (wgs > 0x7fffffffLL) return TC_ERR_SHAPE;

@@ -124,6 +124,28 @@ def test_sequences_of_an_image_share_its_prefix(dtype, each, T):
     check(make(dtype, 64, B, 2, 1, T, T + 60, lens, [int(x) for x in g.integers(0, T + 1, B)], images=2, P=70, seed=each))
 
 
+@pytest.mark.parametrize("dtype,d,H,Hk,each,T,P", [
+    ("bf16", 128, 8, 8, 3, 1, 2100), ("bf16", 64, 16, 16, 8, 2, 1200), ("f16", 64, 8, 8, 12, 5, 1500), ("f16", 128, 16, 4, 10, 1, 1777),
+    ("f32", 64, 8, 8, 9, 1, 1100), ("f32", 128, 4, 4, 20, 2, 500), ("bf16", 64, 8, 8, 33, 16, 300)])
+def test_prefixes_large_enough_to_be_read_once(dtype, d, H, Hk, each, T, P):
+    """From 32 MB on that would be read again: rows of all sequences of an image as one matrix, of up to and over 16 rows."""
+    B = 2 * each
+    g = np.random.default_rng(each + T)
+    assert 2 * (each - 1) * Hk * P * d * 2 * torch.finfo(DTYPES[dtype]).bits // 8 >= 32e6
+    lens = [int(x) for x in g.integers(0, T + 60, B)]
+    q_len = [int(x) for x in g.integers(0, T + 1, B)]
+    check(make(dtype, d, B, H, Hk, T, T + 60, lens, q_len, images=2, P=P, seed=each))
+    check(make(dtype, d, B, H, Hk, T, T + 300, [x + 230 for x in lens], images=2, P=P, seed=each, weights=False))
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("n,P", [(2040, 0), (2048, 0), (2049, 0), (1000, 1040), (1000, 1060), (130, 0), (128, 0), (129, 0), (0, 2000), (1, 127)])
+def test_one_sequence_with_and_without_parts(dtype, d, n, P):
+    # the largest cache of one sweep, and the smallest that is cut
+    check(make(dtype, d, 1, 4, 2, 1, max(n, 1), [n], images=1 if P else 0, P=P))
+    check(make(dtype, d, 1, 2, 2, 3, n + 2, [n], images=1 if P else 0, P=P, weights=False))
+
+
 @pytest.mark.parametrize("T", [1, 6, 90, 300])
 def test_many_rows_without_weights(T):
     check(make("bf16", 128, 2, 4, 2, T, 400, [400, 333], images=1, P=37, weights=False))
