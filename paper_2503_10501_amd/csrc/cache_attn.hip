@@ -252,6 +252,25 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(AttnArgs a, Job first, 
   const int group = item / job.splits / job.tiles, hk = group % a.Hk, b = group / a.Hk;  // (packed: b is the image)
   const int r = tile * 16 + i, row = row_of(a, job, group, min(r, job.rows - 1));  // this lane's row of queries
   const bool mine = r < job.rows;
+  const size_t head = (size_t)group * a.cap, phead = job.prefix ? ((size_t)(job.packed ? b : b / a.each) * a.Hk + hk) * a.P : 0;
+  unsigned char* Ks = cache_smem + wave * S::WAVE;
+  unsigned char* Vs = Ks + FK * S::KLD;
+  u4 kr[NV], vr[NV];
+  // Where the keys are one part each wavefront's first tile is known before the sequence's length is (of which it may hold less, or nothing): it
+  // comes at once, and the queries.
+  const bool ahead = job.splits == 1;
+  if (ahead) {
+    const int tiles = job.prefix ? (a.P + FK - 1) / FK : 0;
+    const bool pre = wave < tiles;
+    const int k0 = (pre ? wave : wave - tiles) * FK, there = pre ? a.P : job.cache ? a.cap : 0;
+    if (k0 < there) fetch_tile<64, VEC>(pre ? a.Kp : a.Kc, pre ? a.Vp : a.Vc, (pre ? phead : head) + k0, there - k0, lane, kr, vr);
+  }
+  frag q[DH / 32];
+  {
+    const u4* Qr = reinterpret_cast<const u4*>(static_cast<const T*>(a.Q) + (size_t)row * DH);
+#pragma unroll
+    for (int s = 0; s < DH / 32; s++) q[s] = frag_of<T>(Qr, 4 * s + g);
+  }
   int n = 0, m = 1, end = 0;
   bool live = mine;
   if (job.cache) {
@@ -271,30 +290,19 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(AttnArgs a, Job first, 
   // tiles of the prefix, then of the cache; this workgroup's share of them, dealt to its wavefronts in turn
   const int np = job.prefix && m > 0 ? (a.P + FK - 1) / FK : 0, all = np + (most + FK - 1) / FK;
   const int t0 = (int)((long long)all * split / job.splits), t1 = (int)((long long)all * (split + 1) / job.splits);
-
-  const size_t head = (size_t)group * a.cap, phead = job.prefix ? ((size_t)(job.packed ? b : b / a.each) * a.Hk + hk) * a.P : 0;
-  unsigned char* Ks = cache_smem + wave * S::WAVE;
-  unsigned char* Vs = Ks + FK * S::KLD;
-  u4 kr[NV], vr[NV];
   auto fetch = [&](int t) {
     const bool pre = t < np;
     const int k0 = (pre ? t : t - np) * FK;
     fetch_tile<64, VEC>(pre ? a.Kp : a.Kc, pre ? a.Vp : a.Vc, (pre ? phead : head) + k0, (pre ? a.P : most) - k0, lane, kr, vr);
   };
 
-  frag q[DH / 32];
-  {
-    const u4* Qr = reinterpret_cast<const u4*>(static_cast<const T*>(a.Q) + (size_t)row * DH);
-#pragma unroll
-    for (int s = 0; s < DH / 32; s++) q[s] = frag_of<T>(Qr, 4 * s + g);
-  }
   f4 o[DT];
 #pragma unroll
   for (int d = 0; d < DT; d++) o[d] = f4{0.f, 0.f, 0.f, 0.f};
   float mx = -INFINITY, sum = 0.f;
 
   int t = t0 + wave;
-  if (t < t1) fetch(t);
+  if (!ahead && t < t1) fetch(t);
   for (; t < t1; t += WAVES) {
     const bool pre = t < np;
     const int k0 = (pre ? t : t - np) * FK, last = pre ? a.P : most;
@@ -576,6 +584,18 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
   const int r0 = tile * ROWS - (job.tiles * ROWS - job.rows) + wave % RW * 32, r = r0 + i, row = row_of(a, job, group, max(r, 0));
   const int ku = KW == 2 ? wave / RW * 32 : 0;  // the wavefront's first key of a tile
   const bool mine = r >= 0, idle = r0 + 31 < 0;
+  const size_t head = (size_t)group * a.cap, phead = job.prefix ? ((size_t)(job.packed ? b : b / a.each) * a.Hk + hk) * a.P : 0;
+  u4 kr[S::NV], vr[S::NV];
+  // Where the keys are one part its first tile is known before the sequence's length is (of which it may hold less): it comes at once, and the
+  // queries.
+  const bool ahead = job.splits == 1;
+  if (ahead) fetch_tile<256, S::VEC>(job.prefix ? a.Kp : a.Kc, job.prefix ? a.Vp : a.Vc, job.prefix ? phead : head, job.prefix ? a.P : a.cap, tid, kr, vr);
+  Wave w;
+  {
+    const u4* Qr = reinterpret_cast<const u4*>(static_cast<const T*>(a.Q) + (size_t)row * DH);
+#pragma unroll
+    for (int c = 0; c < DH / 16; c++) w.q[c].u = Qr[2 * c + half];
+  }
   int m = 1, end = 0;
   bool live = mine;
   if (job.cache) {
@@ -602,8 +622,6 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
   const int np = job.prefix && m > 0 ? (a.P + MK - 1) / MK : 0, all = np + (most + MK - 1) / MK;
   const int t0 = (int)((long long)all * split / job.splits), t1 = (int)((long long)all * (split + 1) / job.splits);
 
-  const size_t head = (size_t)group * a.cap, phead = job.prefix ? ((size_t)(job.packed ? b : b / a.each) * a.Hk + hk) * a.P : 0;
-  u4 kr[S::NV], vr[S::NV];
   auto fetch = [&](int t) {
     const bool pre = t < np;
     const int k0 = (pre ? t : t - np) * MK;
@@ -633,12 +651,6 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
     }
   };
 
-  Wave w;
-  {
-    const u4* Qr = reinterpret_cast<const u4*>(static_cast<const T*>(a.Q) + (size_t)row * DH);
-#pragma unroll
-    for (int c = 0; c < DH / 16; c++) w.q[c].u = Qr[2 * c + half];
-  }
 #pragma unroll
   for (int d = 0; d < DH / 32; d++)
 #pragma unroll
@@ -646,7 +658,7 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
   w.mx = -INFINITY;
   w.sum = 0.f;
   if (t0 < t1) {
-    fetch(t0);
+    if (!ahead) fetch(t0);
     store(t0);
     if (t0 + 1 < t1) fetch(t0 + 1);
     __syncthreads();
