@@ -100,6 +100,20 @@ __device__ inline void wave_lds_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
+// Division of 0 .. 2^31 - 1 by a number that the host knows: with l = ceil(log2 d) and mul = floor(2^32 (2^l - d) / d) + 1 the quotient is
+// (mulhi(n, mul) + n) >> l (Granlund and Montgomery 1994).  What a workgroup does before its first tile is a chain of such divisions and of loads: with
+// the compiler's, 40 instructions each, it took 7000 cycles in the kernel of many rows.
+struct Div {
+  uint32_t d, mul, shift;
+  Div() = default;
+  explicit Div(uint32_t by) : d(by < 1 ? 1 : by), mul(0), shift(0) {
+    while ((1ull << shift) < d) shift++;
+    mul = (uint32_t)(((1ull << 32) * ((1ull << shift) - d)) / d + 1);
+  }
+  __device__ inline int quot(int n) const { return (int)((__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift); }
+  __device__ inline int rem(int n) const { return n - quot(n) * (int)d; }
+};
+
 // What the kernels are told.
 struct AttnArgs {
   const void *Q, *Kp, *Vp, *Kc, *Vc;
@@ -112,6 +126,7 @@ struct AttnArgs {
   float* score; // [row][score_ld]: base-2 scores of the cache's keys, where rows are few
   int score_ld;
   int H, Hk, G, T, R, cap, max_len, each, P;
+  Div by_T, by_R, by_H, by_Hk, by_each;
   int rows;     // all rows: B H T
   int parts;    // parts of the keys of a row
   float scale2; // scale log2(e)
@@ -124,25 +139,39 @@ struct Job {
   int groups, rows, tiles, splits, part0;  // part0: the first of the `splits` parts that this share writes
   bool packed, prefix, cache, many;        // many: by many_kernel
   bool wide;                               // eight wavefronts
+  Div by_splits, by_tiles;
 };
 
 // Row r of a group: its place among all rows.
 __device__ inline int row_of(const AttnArgs& a, const Job& j, int group, int r) {
   if (!j.packed) return group * a.R + r;
-  return ((group / a.Hk * a.each + r / a.R) * a.Hk + group % a.Hk) * a.R + r % a.R;
+  const int image = a.by_Hk.quot(group), sequence = a.by_R.quot(r);
+  return ((image * a.each + sequence) * a.Hk + group - image * a.Hk) * a.R + r - sequence * a.R;
 }
 
-// Row r of a sequence: what it sees of the cache.  Rows behind the last token see what that one sees; nothing of them is kept.
-__device__ inline int seen(const AttnArgs& a, int r, int n, int m) {
-  const int t = min(r % a.T, m - 1);
-  return clamp_len(n - m + t + 1, n);
+// Tokens of a sequence in this call, and slots in use.
+__device__ inline int tokens_of(const AttnArgs& a, int b) { return a.q_len ? clamp_len(a.q_len[b], a.T) : a.T; }
+__device__ inline int slots_of(const AttnArgs& a, int b) { return clamp_len(a.len[b], a.max_len); }
+
+// What token t of m sees of the n slots.  Rows behind the last token see what that one sees; nothing of them is kept.
+__device__ inline int seen(int t, int n, int m) { return clamp_len(n - m + min(t, m - 1) + 1, n); }
+
+// The least and the most that rows first .. last of a sequence see.
+__device__ inline void seen_by(const AttnArgs& a, int first, int last, int n, int m, int& least, int& most) {
+  const int g0 = a.by_T.quot(first), g1 = a.by_T.quot(last);
+  least = seen(g0 == g1 ? first - g0 * a.T : 0, n, m);
+  most = seen(g0 == g1 ? last - g0 * a.T : a.T - 1, n, m);
 }
 
-// Where row `row` (of all rows) of the output lies.
-__device__ inline size_t out_row(const AttnArgs& a, int row, int dh) {
-  const int t = row % a.T, h = row / a.T % a.H, b = row / a.T / a.H;
-  return (((size_t)b * a.T + t) * a.H + h) * dh;
+// Share `split` of `all` tiles.
+__device__ inline void share_of(const Job& j, int all, int split, int& t0, int& t1) {
+  const int q = j.by_splits.quot(all), more = all - q * j.splits;
+  t0 = q * split + min(split, more);
+  t1 = t0 + q + (split < more ? 1 : 0);
 }
+
+// Where token t of head h lies in the output.
+__device__ inline size_t out_row(const AttnArgs& a, int b, int h, int t, int dh) { return (((size_t)b * a.T + t) * a.H + h) * dh; }
 
 template <typename T>
 __device__ inline bool not_finite(T v) {
@@ -209,7 +238,7 @@ __device__ inline void add_weights(const AttnArgs& a, int group, int k, int n, i
   f4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
   for (int r = 0; r < a.R; r++) {
-    const int end = seen(a, r, n, m);
+    const int end = seen(a.by_T.rem(r), n, m);
     f4 s = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
     if (k < end && lse[r] < INFINITY) s = *reinterpret_cast<const f4*>(a.score + (size_t)(group * a.R + r) * a.score_ld + k);
 #pragma unroll
@@ -248,11 +277,12 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(AttnArgs a, Job first, 
   const bool other = blockIdx.x >= in_first;
   const Job job = other ? second : first;
   const unsigned item = blockIdx.x - (other ? in_first : 0);
-  const int split = item % job.splits, tile = item / job.splits % job.tiles;
-  const int group = item / job.splits / job.tiles, hk = group % a.Hk, b = group / a.Hk;  // (packed: b is the image)
+  const int at_tile = job.by_splits.quot(item), split = item - at_tile * job.splits;
+  const int group = job.by_tiles.quot(at_tile), tile = at_tile - group * job.tiles;
+  const int b = a.by_Hk.quot(group), hk = group - b * a.Hk;  // (packed: b is the image)
   const int r = tile * 16 + i, row = row_of(a, job, group, min(r, job.rows - 1));  // this lane's row of queries
   const bool mine = r < job.rows;
-  const size_t head = (size_t)group * a.cap, phead = job.prefix ? ((size_t)(job.packed ? b : b / a.each) * a.Hk + hk) * a.P : 0;
+  const size_t head = (size_t)group * a.cap, phead = job.prefix ? ((size_t)(job.packed ? b : a.by_each.quot(b)) * a.Hk + hk) * a.P : 0;
   unsigned char* Ks = cache_smem + wave * S::WAVE;
   unsigned char* Vs = Ks + FK * S::KLD;
   u4 kr[NV], vr[NV];
@@ -271,25 +301,20 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(AttnArgs a, Job first, 
 #pragma unroll
     for (int s = 0; s < DH / 32; s++) q[s] = frag_of<T>(Qr, 4 * s + g);
   }
-  int n = 0, m = 1, end = 0;
+  int n = 0, m = 1, end = 0, most = 0, least = 0;
   bool live = mine;
   if (job.cache) {
-    n = clamp_len(a.len[b], a.max_len);
-    m = a.q_len ? clamp_len(a.q_len[b], a.T) : a.T;
-    live = mine && r % a.T < m;
-    end = m > 0 ? seen(a, min(r, a.R - 1), n, m) : 0;
+    n = slots_of(a, b);
+    m = tokens_of(a, b);
+    const int tok = a.by_T.rem(min(r, a.R - 1));
+    live = mine && tok < m;
+    end = seen(tok, n, m);
+    seen_by(a, tile * 16, min(tile * 16 + 15, a.R - 1), n, m, least, most);
   }
-  int most = end, least = end;
-#pragma unroll
-  for (int o = 1; o < 16; o <<= 1) {
-    most = max(most, __shfl_xor(most, o, 64));
-    least = min(least, __shfl_xor(least, o, 64));
-  }
-  most = __builtin_amdgcn_readfirstlane(most);
-  least = __builtin_amdgcn_readfirstlane(least);
   // tiles of the prefix, then of the cache; this workgroup's share of them, dealt to its wavefronts in turn
-  const int np = job.prefix && m > 0 ? (a.P + FK - 1) / FK : 0, all = np + (most + FK - 1) / FK;
-  const int t0 = (int)((long long)all * split / job.splits), t1 = (int)((long long)all * (split + 1) / job.splits);
+  const int np = job.prefix && m > 0 ? (a.P + FK - 1) / FK : 0, all = m > 0 ? np + (most + FK - 1) / FK : 0;
+  int t0, t1;
+  share_of(job, all, split, t0, t1);
   auto fetch = [&](int t) {
     const bool pre = t < np;
     const int k0 = (pre ? t : t - np) * FK;
@@ -440,12 +465,13 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(AttnArgs a, Job first, 
     f4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < WAVES; w++) v += *reinterpret_cast<const f4*>(cache_smem + w * S::WAVE + (rr * (DH + 4) + 4 * c) * 4);
-    const int to = row_of(a, job, group, tile * 16 + rr);
     if (a.parts > 1) {
+      const int to = row_of(a, job, group, tile * 16 + rr);
       *reinterpret_cast<f4*>(a.part + ((size_t)(job.part0 + split) * a.rows + to) * DH + 4 * c) = v;
     } else {
       v = row_sum[rr] < INFINITY || row_sum[rr] != row_sum[rr] ? v / row_sum[rr] : f4{0.f, 0.f, 0.f, 0.f};
-      T* out = static_cast<T*>(a.O) + out_row(a, to, DH) + 4 * c;
+      const int head_of = a.by_T.quot(tile * 16 + rr);
+      T* out = static_cast<T*>(a.O) + out_row(a, b, hk * a.G + head_of, tile * 16 + rr - head_of * a.T, DH) + 4 * c;
 #pragma unroll
       for (int e = 0; e < 4; e++) out[e] = Vec16<T>::round(v[e]);
     }
@@ -573,18 +599,18 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
   typedef ManyWave<T, DH, KW> Wave;
   constexpr int ROWS = MROWS / KW, RW = 4 / KW;  // rows of the workgroup, wavefronts that share them
   extern __shared__ __attribute__((aligned(16))) unsigned char cache_smem[];
-  __shared__ int ends[2][4], flag[3];
+  __shared__ int flag[3];
   __shared__ size_t places[4][32];  // of rows in the output
   int group, item;
   if (!group_on_xcd(blockIdx.x, job.tiles * job.splits, job.groups, &group, &item)) return;
-  const int split = item % job.splits, tile = job.tiles - 1 - item / job.splits;  // (the rows that see the most first)
+  const int back = job.by_splits.quot(item), split = item - back * job.splits, tile = job.tiles - 1 - back;  // (the rows that see the most first)
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, i = lane & 31;
-  const int hk = group % a.Hk, b = group / a.Hk;  // (packed: b is the image)
+  const int b = a.by_Hk.quot(group), hk = group - b * a.Hk;  // (packed: b is the image)
   // The tiles are laid so that the last one is full: the empty rows are in the first one, which sees the fewest keys.
-  const int r0 = tile * ROWS - (job.tiles * ROWS - job.rows) + wave % RW * 32, r = r0 + i, row = row_of(a, job, group, max(r, 0));
+  const int tile0 = tile * ROWS - (job.tiles * ROWS - job.rows), r0 = tile0 + wave % RW * 32, r = r0 + i, row = row_of(a, job, group, max(r, 0));
   const int ku = KW == 2 ? wave / RW * 32 : 0;  // the wavefront's first key of a tile
   const bool mine = r >= 0, idle = r0 + 31 < 0;
-  const size_t head = (size_t)group * a.cap, phead = job.prefix ? ((size_t)(job.packed ? b : b / a.each) * a.Hk + hk) * a.P : 0;
+  const size_t head = (size_t)group * a.cap, phead = job.prefix ? ((size_t)(job.packed ? b : a.by_each.quot(b)) * a.Hk + hk) * a.P : 0;
   u4 kr[S::NV], vr[S::NV];
   // Where the keys are one part its first tile is known before the sequence's length is (of which it may hold less): it comes at once, and the
   // queries.
@@ -596,31 +622,23 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
 #pragma unroll
     for (int c = 0; c < DH / 16; c++) w.q[c].u = Qr[2 * c + half];
   }
-  int m = 1, end = 0;
+  int m = 1, end = 0, most = 0, least = 0, wave_most = 0, wave_least = 0, head_of = 0, tok = 0;
   bool live = mine;
   if (job.cache) {
-    const int n = clamp_len(a.len[b], a.max_len);
-    m = a.q_len ? clamp_len(a.q_len[b], a.T) : a.T;
-    live = mine && r % a.T < m;
-    end = m > 0 ? seen(a, max(r, 0), n, m) : 0;
-  }
-  int most = end, least = end;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    most = max(most, __shfl_xor(most, o, 64));
-    least = min(least, __shfl_xor(least, o, 64));
-  }
-  const int wave_most = __builtin_amdgcn_readfirstlane(most), wave_least = __builtin_amdgcn_readfirstlane(least);
-  if (lane == 0) {
-    ends[0][wave] = most;
-    ends[1][wave] = least;
+    const int n = slots_of(a, b);
+    m = tokens_of(a, b);
+    head_of = a.by_T.quot(max(r, 0));
+    tok = max(r, 0) - head_of * a.T;
+    live = mine && tok < m;
+    end = seen(tok, n, m);
+    seen_by(a, max(tile0, 0), tile0 + ROWS - 1, n, m, least, most);
+    seen_by(a, max(r0, 0), max(r0 + 31, 0), n, m, wave_least, wave_most);
   }
   if (tid < 3) flag[tid] = 0;
   __syncthreads();
-  most = __builtin_amdgcn_readfirstlane(max(max(ends[0][0], ends[0][1]), max(ends[0][2], ends[0][3])));
-  least = __builtin_amdgcn_readfirstlane(min(min(ends[1][0], ends[1][1]), min(ends[1][2], ends[1][3])));
-  const int np = job.prefix && m > 0 ? (a.P + MK - 1) / MK : 0, all = np + (most + MK - 1) / MK;
-  const int t0 = (int)((long long)all * split / job.splits), t1 = (int)((long long)all * (split + 1) / job.splits);
+  const int np = job.prefix && m > 0 ? (a.P + MK - 1) / MK : 0, all = m > 0 ? np + (most + MK - 1) / MK : 0;
+  int t0, t1;
+  share_of(job, all, split, t0, t1);
 
   auto fetch = [&](int t) {
     const bool pre = t < np;
@@ -719,7 +737,7 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
   const bool sees = live && a.P + end > 0;
   const float inv = 1.f / total;
   unsigned char* Os = cache_smem + 2 * 64 * (DH / 2 + 2) * 4 * (KW - 1) + wave * 32 * S::KLD;
-  if (half == 0) places[wave][i] = out_row(a, row, DH);
+  if (half == 0) places[wave][i] = out_row(a, b, hk * a.G + head_of, tok, DH);
 #pragma unroll
   for (int d = 0; d < DH / 32; d++)
 #pragma unroll
@@ -751,9 +769,9 @@ __device__ inline void row_stats(const AttnArgs& a, int row, int lane, float& re
   total = wave_sum(total);
 }
 __device__ inline bool row_live(const AttnArgs& a, int row, bool& sees) {
-  const int b = row / a.T / a.H, t = row % a.T;
-  const int n = clamp_len(a.len[b], a.max_len), m = a.q_len ? clamp_len(a.q_len[b], a.T) : a.T;
-  sees = t < m && a.P + clamp_len(n - m + t + 1, n) > 0;
+  const int head = a.by_T.quot(row), t = row - head * a.T, b = a.by_H.quot(head);
+  const int n = slots_of(a, b), m = tokens_of(a, b);
+  sees = t < m && a.P + seen(t, n, m) > 0;
   return t < m;
 }
 
@@ -789,7 +807,8 @@ __device__ inline void join_row(const AttnArgs& a, int row, float* lds) {
     }
   }
   if (p == 0) {
-    T* out = static_cast<T*>(a.O) + out_row(a, row, DH) + 4 * c;
+    const int head = a.by_T.quot(row), b = a.by_H.quot(head);
+    T* out = static_cast<T*>(a.O) + out_row(a, b, head - b * a.H, row - head * a.T, DH) + 4 * c;
 #pragma unroll
     for (int e = 0; e < 4; e++) out[e] = Vec16<T>::round(sees ? v[e] / total : 0.f);
   }
@@ -817,7 +836,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
 // probabilities of a sequence's rows to GW slots of a head.
 constexpr int GW = 1024;
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void join_gather_kernel(AttnArgs a, int row_wgs, int chunks) {
+__global__ __launch_bounds__(256) void join_gather_kernel(AttnArgs a, int row_wgs, Div by_chunks) {
   __shared__ float lse[16];
   __shared__ __attribute__((aligned(16))) float lds[4 * DH];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -825,8 +844,8 @@ __global__ __launch_bounds__(256) void join_gather_kernel(AttnArgs a, int row_wg
     join_rows<T, DH>(a, lds);
     return;
   }
-  const unsigned item = blockIdx.x - row_wgs, bh = item / chunks;
-  const int b = bh / a.Hk, first = (int)(item % chunks) * GW, n = clamp_len(a.len[b], a.max_len);
+  const int item = blockIdx.x - row_wgs, bh = by_chunks.quot(item);
+  const int b = a.by_Hk.quot(bh), first = (item - bh * (int)by_chunks.d) * GW, n = slots_of(a, b);
   if (first >= n) return;
   for (int r = wave; r < a.R; r += 4) {
     const int row = bh * a.R + r;
@@ -838,18 +857,17 @@ __global__ __launch_bounds__(256) void join_gather_kernel(AttnArgs a, int row_wg
   }
   __syncthreads();
   const int k = first + 4 * (int)threadIdx.x;
-  if (k < n) add_weights(a, bh, k, n, a.q_len ? clamp_len(a.q_len[b], a.T) : a.T, lse);
+  if (k < n) add_weights(a, bh, k, n, tokens_of(a, b), lse);
 }
 
 // What slots gather: 16 keys per wavefront, kept in registers; the rows of queries pass by, 16 at a time.
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void gather_kernel(AttnArgs a, int chunks) {
+__global__ __launch_bounds__(256) void gather_kernel(AttnArgs a, Div by_chunks) {
   typedef Mma<T> M;
   typedef typename M::frag frag;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-  const unsigned bh = blockIdx.x / chunks;
-  const int b = bh / a.Hk, k0 = (int)(blockIdx.x % chunks) * 64 + wave * 16;
-  const int n = clamp_len(a.len[b], a.max_len), m = a.q_len ? clamp_len(a.q_len[b], a.T) : a.T;
+  const int bh = by_chunks.quot(blockIdx.x), b = a.by_Hk.quot(bh), k0 = (int)(blockIdx.x - bh * by_chunks.d) * 64 + wave * 16;
+  const int n = slots_of(a, b), m = tokens_of(a, b);
   if (k0 >= n || m == 0) return;
   frag k[DH / 32];
   const u4* Kr = reinterpret_cast<const u4*>(static_cast<const T*>(a.Kc) + ((size_t)bh * a.cap + min(k0 + i, n - 1)) * DH);
@@ -865,7 +883,7 @@ __global__ __launch_bounds__(256) void gather_kernel(AttnArgs a, int chunks) {
 #pragma unroll
     for (int c = 0; c < DH / 32; c++) s = M::mul(k[c], frag_of<T>(Qr, 4 * c + g), s);
     const float lse = r0 + i < a.R ? a.lse[row] : INFINITY;
-    const int end = seen(a, r, n, m);
+    const int end = seen(a.by_T.rem(r), n, m);
 #pragma unroll
     for (int e = 0; e < 4; e++) acc[e] += lse < INFINITY && k0 + 4 * g + e < end ? exp2_fast(s[e] * a.scale2 - lse) : 0.f;
   }
@@ -885,7 +903,8 @@ constexpr int FEW_ROWS = 16;
 static Job make_job(const CachePlan& pl, int groups, int rows, int keys, bool packed, bool prefix, bool cache, bool alone) {
   const bool many = rows > FEW_ROWS && pl.esize == 2;
   const int per = !many ? FEW_ROWS : rows <= MROWS / 2 ? MROWS / 2 : MROWS, tile = many ? MK : FK, least = many ? 2 : 4;
-  Job j = {groups, rows, (rows + per - 1) / per, 1, 0, packed, prefix, cache, many, false};
+  Job j = {groups, rows, (rows + per - 1) / per, 1, 0, packed, prefix, cache, many, false, Div(1), Div(1)};
+  j.by_tiles = Div((uint32_t)j.tiles);
   const long long items = (long long)groups * j.tiles, tiles = (keys + tile - 1) / tile + (prefix && cache ? 1 : 0);
   // Few rows on a part of the chip, up to 768 keys: eight wavefronts take all keys, and nothing has to be joined.  (One sequence, 32 heads,
   // us in one sweep and in parts: 640 keys 10.5 and 11.9, 1000 14.3 and 12.5, 2000 21 and 15.)
@@ -902,6 +921,7 @@ static Job make_job(const CachePlan& pl, int groups, int rows, int keys, bool pa
     if (t > s) s = t;
   }
   j.splits = s < 1 ? 1 : (int)s;
+  j.by_splits = Div((uint32_t)j.splits);
   return j;
 }
 struct Cut {
@@ -984,11 +1004,11 @@ static int attention_launch(const CachePlan& pl, AttnArgs a, hipStream_t st) {
     chunks = (pl.max_len + GW - 1) / GW;
     const long long wgs = row_wgs + chunks * pl.B * pl.Hk;
     if (wgs > 0x7fffffffLL) return TC_ERR_SHAPE;
-    join_gather_kernel<T, DH><<<(unsigned)wgs, 256, 0, st>>>(a, row_wgs, (int)chunks);
+    join_gather_kernel<T, DH><<<(unsigned)wgs, 256, 0, st>>>(a, row_wgs, Div((uint32_t)chunks));
     return check_launch();
   }
   if (a.parts > 1) join_kernel<T, DH><<<row_wgs, 256, 0, st>>>(a);
-  if (a.weight) gather_kernel<T, DH><<<(unsigned)(chunks * pl.B * pl.Hk), 256, 0, st>>>(a, (int)chunks);
+  if (a.weight) gather_kernel<T, DH><<<(unsigned)(chunks * pl.B * pl.Hk), 256, 0, st>>>(a, Div((uint32_t)chunks));
   return check_launch();
 }
 
@@ -1011,6 +1031,7 @@ extern "C" int tc_cache_attention(const tc_cache* c, const void* Q, const void* 
   AttnArgs a = {};
   a.Q = Q; a.Kp = K_prefix; a.Vp = V_prefix; a.Kc = K_cache; a.Vc = V_cache; a.len = len; a.q_len = q_len; a.O = O; a.weight = weight;
   a.H = pl.H; a.Hk = pl.Hk; a.G = pl.G; a.T = pl.T; a.R = pl.R; a.cap = pl.cap; a.max_len = pl.max_len; a.each = pl.each; a.P = pl.P;
+  a.by_T = Div(a.T); a.by_R = Div(a.R); a.by_H = Div(a.H); a.by_Hk = Div(a.Hk); a.by_each = Div(a.each);
   a.rows = pl.B * pl.H * pl.T;
   a.scale2 = pl.scale * 1.44269504088896340736f;
   int bits = 1;  // 2^bits is more than twice the keys of a row
