@@ -94,6 +94,12 @@ __device__ inline float col_sum(float x) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// The value of the lane that a data-parallel permutation pairs this one with, within 16 lanes.
+template <int CTRL>
+__device__ inline float lane_of(float x) {
+  return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), CTRL, 0xF, 0xF, false));
+}
+
 // LDS that only one wavefront uses: its accesses are executed in order, and the compiler keeps that order here.
 __device__ inline void wave_lds_order() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -232,17 +238,21 @@ __device__ __forceinline__ void zero_behind(int there, int id, u4 (&vr)[NV]) {
 }
 
 // Slots k .. k + 3 of a sequence and head gather the probabilities of its few rows, from the scores that were kept.  A row's scores are there up to
-// the tile that the last row sees; behind what the row sees they are not looked at.
+// the tile that the last row sees; what lies behind what the row sees is read and left out (loads under conditions would wait for one another:
+// 2 sequences of 10 rows 4.8 us of 11.5).
 __device__ inline void add_weights(const AttnArgs& a, int group, int k, int n, int m, const float* lse) {
   float* w = a.weight + (size_t)group * a.cap + k;
+  const float* score = a.score + (size_t)group * a.R * a.score_ld + k;
   f4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
   for (int r = 0; r < a.R; r++) {
-    const int end = seen(a.by_T.rem(r), n, m);
-    f4 s = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    if (k < end && lse[r] < INFINITY) s = *reinterpret_cast<const f4*>(a.score + (size_t)(group * a.R + r) * a.score_ld + k);
+    const int end = lse[r] == INFINITY ? 0 : seen(a.by_T.rem(r), n, m);
+    const f4 s = *reinterpret_cast<const f4*>(score + (size_t)r * a.score_ld);
 #pragma unroll
-    for (int e = 0; e < 4; e++) acc[e] += k + e < end && lse[r] < INFINITY ? exp2_fast(s[e] - lse[r]) : 0.f;
+    for (int e = 0; e < 4; e++) {
+      const float p = exp2_fast(s[e] - lse[r]);
+      acc[e] += k + e < end ? p : 0.f;
+    }
   }
 #pragma unroll
   for (int e = 0; e < 4; e++)
@@ -491,7 +501,7 @@ constexpr int MK = 64, MROWS = 128;
 template <int DH>
 struct ManyShape {
   static constexpr int VEC = DH / 8, NV = MK * VEC / 256;         // 16-byte vectors of a row, of a thread
-  static constexpr int KLD = DH * 2 + 16, VLD = DH * 2 + 64;      // rows in LDS: 16 lanes of a read meet other banks
+  static constexpr int KLD = DH * 2 + 16, VLD = DH * 2 + 32;      // rows in LDS: 16 lanes of a read meet other banks; heads of 64: four workgroups fit
   static constexpr int STAGE = MK * (KLD + VLD), LDS = 2 * STAGE;
   static_assert(4 * 32 * KLD <= LDS && 2 * 64 * (DH / 2 + 2) * 4 + 2 * 32 * KLD <= LDS, "outputs take the place of the tiles");
 };
@@ -860,40 +870,69 @@ __global__ __launch_bounds__(256) void join_gather_kernel(AttnArgs a, int row_wg
   if (k < n) add_weights(a, bh, k, n, tokens_of(a, b), lse);
 }
 
-// What slots gather: 16 keys per wavefront, kept in registers; the rows of queries pass by, 16 at a time.
+// What slots gather where rows are many: 32 keys per wavefront, kept in registers; the rows of queries pass by, GR of 16 at a time, whose loads are
+// issued together.  The keys and the first rows come before the length is known.
+constexpr int GR = 2, GK = 128;  // (GK: keys of a workgroup)
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void gather_kernel(AttnArgs a, Div by_chunks) {
   typedef Mma<T> M;
   typedef typename M::frag frag;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-  const int bh = by_chunks.quot(blockIdx.x), b = a.by_Hk.quot(bh), k0 = (int)(blockIdx.x - bh * by_chunks.d) * 64 + wave * 16;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
+  const int bh = by_chunks.quot(blockIdx.x), b = a.by_Hk.quot(bh), k0 = (int)(blockIdx.x - bh * by_chunks.d) * GK + wave * 32;
+  frag k[2][DH / 32], q[GR][DH / 32];
+  float lse[GR];
+#pragma unroll
+  for (int u = 0; u < 2; u++) {
+    const u4* Kr = reinterpret_cast<const u4*>(static_cast<const T*>(a.Kc) + ((size_t)bh * a.cap + min(k0 + 16 * u + i, a.cap - 1)) * DH);
+#pragma unroll
+    for (int s = 0; s < DH / 32; s++) k[u][s] = frag_of<T>(Kr, 4 * s + g);
+  }
+  auto load = [&](int r0) {
+#pragma unroll
+    for (int x = 0; x < GR; x++) {
+      const int r = r0 + 16 * x + i;
+      const size_t row = (size_t)bh * a.R + min(r, a.R - 1);
+      const u4* Qr = reinterpret_cast<const u4*>(static_cast<const T*>(a.Q) + row * DH);
+#pragma unroll
+      for (int c = 0; c < DH / 32; c++) q[x][c] = frag_of<T>(Qr, 4 * c + g);
+      lse[x] = a.lse[row];
+      if (r >= a.R) lse[x] = INFINITY;
+    }
+  };
+  load(0);
   const int n = slots_of(a, b), m = tokens_of(a, b);
   if (k0 >= n || m == 0) return;
-  frag k[DH / 32];
-  const u4* Kr = reinterpret_cast<const u4*>(static_cast<const T*>(a.Kc) + ((size_t)bh * a.cap + min(k0 + i, n - 1)) * DH);
+  f4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+  for (int r0 = 0; r0 < a.R; r0 += 16 * GR) {
+    if (r0 > 0) load(r0);
 #pragma unroll
-  for (int s = 0; s < DH / 32; s++) k[s] = frag_of<T>(Kr, 4 * s + g);
-  f4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int r0 = 0; r0 < a.R; r0 += 16) {
-    const int r = min(r0 + i, a.R - 1);
-    const size_t row = (size_t)bh * a.R + r;
-    const u4* Qr = reinterpret_cast<const u4*>(static_cast<const T*>(a.Q) + row * DH);
-    f4 s = {0.f, 0.f, 0.f, 0.f};
+    for (int x = 0; x < GR; x++) {
+      const int end = lse[x] == INFINITY ? 0 : seen(a.by_T.rem(min(r0 + 16 * x + i, a.R - 1)), n, m);
 #pragma unroll
-    for (int c = 0; c < DH / 32; c++) s = M::mul(k[c], frag_of<T>(Qr, 4 * c + g), s);
-    const float lse = r0 + i < a.R ? a.lse[row] : INFINITY;
-    const int end = seen(a.by_T.rem(r), n, m);
+      for (int u = 0; u < 2; u++) {
+        f4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < 4; e++) acc[e] += lse < INFINITY && k0 + 4 * g + e < end ? exp2_fast(s[e] * a.scale2 - lse) : 0.f;
+        for (int c = 0; c < DH / 32; c++) s = M::mul(k[u][c], q[x][c], s);
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          const float p = exp2_fast(s[e] * a.scale2 - lse[x]);
+          acc[u][e] += k0 + 16 * u + 4 * g + e < end ? p : 0.f;
+        }
+      }
+    }
   }
+  // the rows' sums: lane i = 0 .. 3 of each 16 takes key 4 g + i
 #pragma unroll
-  for (int e = 0; e < 4; e++)
+  for (int u = 0; u < 2; u++) {
 #pragma unroll
-    for (int o = 1; o < 16; o <<= 1) acc[e] += __shfl_xor(acc[e], o, 64);
-  if (i < 4 && k0 + 4 * g + i < n) {
-    const float x = i == 0 ? acc[0] : i == 1 ? acc[1] : i == 2 ? acc[2] : acc[3];
-    a.weight[(size_t)bh * a.cap + k0 + 4 * g + i] += x;
+    for (int e = 0; e < 4; e++) {
+      acc[u][e] += lane_of<0xB1>(acc[u][e]);   // L ^ 1
+      acc[u][e] += lane_of<0x4E>(acc[u][e]);   // L ^ 2
+      acc[u][e] += lane_of<0x141>(acc[u][e]);  // 7 - L of each 8
+      acc[u][e] += lane_of<0x140>(acc[u][e]);  // 15 - L of each 16
+    }
+    const int at = k0 + 16 * u + 4 * g + i;
+    if (i < 4 && at < n) a.weight[(size_t)bh * a.cap + at] += i == 0 ? acc[u][0] : i == 1 ? acc[u][1] : i == 2 ? acc[u][2] : acc[u][3];
   }
 }
 
@@ -975,7 +1014,7 @@ template <typename T, int DH>
 static int attention_launch(const CachePlan& pl, AttnArgs a, hipStream_t st) {
   const Cut cut = make_cut(pl, pl.max_len);
   a.parts = cut.parts;
-  long long chunks = (pl.max_len + 63) / 64;
+  long long chunks = (pl.max_len + GK - 1) / GK;
   if (workgroups(cut.job[0]) + workgroups(cut.job[1]) > 0x7fffffffLL || (a.weight && chunks * pl.B * pl.Hk > 0x7fffffffLL)) return TC_ERR_SHAPE;
   Job few[2] = {};
   int nf = 0;
