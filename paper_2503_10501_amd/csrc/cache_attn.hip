@@ -936,6 +936,112 @@ __global__ __launch_bounds__(256) void gather_kernel(AttnArgs a, Div by_chunks) 
   }
 }
 
+// ... of more rows than GATHER_ROWS in 16-bit storage: 128 keys a workgroup, 32 of them in a wavefront's registers as the operand of 32 x 32 tiles; 64
+// rows at a time pass through LDS for all four (two stages, as in many_kernel).  Rows that see none of the keys are not fetched.
+constexpr int GATHER_ROWS = 64;
+template <typename T, int DH>
+__global__ __launch_bounds__(256, 2) void gather_many_kernel(AttnArgs a, Div by_chunks) {
+  typedef Mma<T> M;
+  typedef typename M::frag frag;
+  constexpr int VEC = DH / 8, NV = 64 * VEC / 256, LD = DH * 2 + 16;
+  __shared__ __attribute__((aligned(16))) unsigned char rows[2][64 * LD];
+  __shared__ float lses[2][64], sums[4][32];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, i = lane & 31;
+  const int bh = by_chunks.quot(blockIdx.x), b = a.by_Hk.quot(bh), kmin = (int)(blockIdx.x - bh * by_chunks.d) * GK, k0 = kmin + wave * 32;
+  frag k[DH / 16];
+  const u4* Kr = reinterpret_cast<const u4*>(static_cast<const T*>(a.Kc) + ((size_t)bh * a.cap + min(k0 + i, a.cap - 1)) * DH);
+#pragma unroll
+  for (int c = 0; c < DH / 16; c++) k[c].u = Kr[2 * c + half];
+  const int n = slots_of(a, b), m = tokens_of(a, b), tiles = (a.R + 63) / 64;
+  if (kmin >= n || m == 0) return;
+  // the next tile from t on of which some row sees the first key
+  auto next = [&](int t) {
+    for (; t < tiles; t++) {
+      int least, most;
+      seen_by(a, t * 64, min(t * 64 + 63, a.R - 1), n, m, least, most);
+      if (most > kmin) break;
+    }
+    return t;
+  };
+  u4 qr[NV];
+  float lse = INFINITY;
+  auto fetch = [&](int t) {
+    const u4* Qr = reinterpret_cast<const u4*>(static_cast<const T*>(a.Q) + ((size_t)bh * a.R + t * 64) * DH);
+    const int there = min(64, a.R - t * 64) * VEC - 1;
+#pragma unroll
+    for (int j = 0; j < NV; j++) qr[j] = Qr[min(tid + 256 * j, there)];
+    const int r = t * 64 + (tid & 63);
+    lse = a.lse[(size_t)bh * a.R + min(r, a.R - 1)];
+    if (r >= a.R) lse = INFINITY;
+  };
+  auto store = [&](int stage) {
+#pragma unroll
+    for (int j = 0; j < NV; j++) {
+      const int at = tid + 256 * j;
+      *reinterpret_cast<u4*>(rows[stage] + at / VEC * LD + at % VEC * 16) = qr[j];
+    }
+    if (tid < 64) lses[stage][tid] = lse;
+  };
+  float acc[16];
+#pragma unroll
+  for (int e = 0; e < 16; e++) acc[e] = 0.f;
+  int t = next(0), stage = 0;
+  if (t < tiles) {
+    fetch(t);
+    store(0);
+  }
+  int t2 = next(t + 1);
+  if (t2 < tiles) fetch(t2);
+  __syncthreads();
+  while (t < tiles) {
+#pragma unroll
+    for (int u = 0; u < 2; u++) {
+      const int r = t * 64 + 32 * u + i;
+      const float l = lses[stage][32 * u + i];
+      const int end = l == INFINITY ? 0 : seen(a.by_T.rem(min(r, a.R - 1)), n, m);
+      if (!__ballot(end > k0)) continue;
+      f16v s;
+#pragma unroll
+      for (int e = 0; e < 16; e++) s[e] = 0.f;
+      const unsigned char* qrow = rows[stage] + (32 * u + i) * LD + 16 * half;
+#pragma unroll
+      for (int c = 0; c < DH / 16; c++) {
+        frag q;
+        q.u = *reinterpret_cast<const u4*>(qrow + 32 * c);
+        s = M::mul32(k[c], q, s);
+      }
+      if (!__ballot(end < k0 + 32)) {
+#pragma unroll
+        for (int e = 0; e < 16; e++) acc[e] += exp2_fast(fmaf(s[e], a.scale2, -l));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; e++) {
+          const float p = exp2_fast(fmaf(s[e], a.scale2, -l));
+          acc[e] += k0 + 8 * (e >> 2) + 4 * half + (e & 3) < end ? p : 0.f;
+        }
+      }
+    }
+    if (t2 < tiles) store(stage ^ 1);  // (last read before the last barrier)
+    __syncthreads();
+    t = t2;
+    stage ^= 1;
+    t2 = next(t + 1);
+    if (t2 < tiles) fetch(t2);
+  }
+#pragma unroll
+  for (int e = 0; e < 16; e++) {
+    float x = acc[e];
+    x += lane_of<0xB1>(x);
+    x += lane_of<0x4E>(x);
+    x += lane_of<0x141>(x);
+    x += lane_of<0x140>(x);
+    const u2 w = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    if (i == 0) sums[wave][8 * (e >> 2) + 4 * half + (e & 3)] = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+  }
+  wave_lds_order();
+  if (lane < 32 && k0 + lane < n) a.weight[(size_t)bh * a.cap + k0 + lane] += sums[wave][lane];
+}
+
 // How a call is cut.  The prefix of an image's sequences is read once for all of them where the rows of one sequence do not fill a
 // tile by themselves; else a sequence's rows go over its prefix and its cache in one sweep.
 constexpr int FEW_ROWS = 16;
@@ -1047,7 +1153,15 @@ static int attention_launch(const CachePlan& pl, AttnArgs a, hipStream_t st) {
     return check_launch();
   }
   if (a.parts > 1) join_kernel<T, DH><<<row_wgs, 256, 0, st>>>(a);
-  if (a.weight) gather_kernel<T, DH><<<(unsigned)(chunks * pl.B * pl.Hk), 256, 0, st>>>(a, Div((uint32_t)chunks));
+  if (a.weight) {
+    const unsigned wgs = (unsigned)(chunks * pl.B * pl.Hk);
+    bool done = false;
+    if constexpr (sizeof(T) == 2) {
+      done = pl.R > GATHER_ROWS;
+      if (done) gather_many_kernel<T, DH><<<wgs, 256, 0, st>>>(a, Div((uint32_t)chunks));
+    }
+    if (!done) gather_kernel<T, DH><<<wgs, 256, 0, st>>>(a, Div((uint32_t)chunks));
+  }
   return check_launch();
 }
 
