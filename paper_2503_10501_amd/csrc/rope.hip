@@ -145,122 +145,87 @@ struct RopeItem {
   }
 };
 
-// Token, head and item of a thread: items fastest, then `groups` heads side by side, then tokens.
+// Token, head and item of a thread: items fastest, then heads, then tokens.
 struct RopeThread {
   long long token;
   int head, item;
 };
-__device__ inline RopeThread rope_thread(int items, int groups) {
-  const unsigned per = (unsigned)(items * groups);
+__device__ inline RopeThread rope_thread(int items, int heads) {
+  const unsigned per = (unsigned)(items * heads);
   const unsigned long long at = (unsigned long long)blockIdx.x * 256;
   const unsigned long long t0 = at / per;
   const unsigned off = (unsigned)(at - t0 * per) + threadIdx.x, in = off % per;
   return {(long long)(t0 + off / per), (int)(in / (unsigned)items), (int)(in % (unsigned)items)};
 }
 
-// A thread keeps its item's part of the tables for PER heads: heads of a token read them once.
-template <typename T, bool INTER, bool VEC, int PER>
+// One item a thread: the memory's rate bounds it, and what a thread reads of the tables its neighbours' heads have just read.  (64 x 128 tokens, 32 heads
+// of 128, bf16: 24.7 us, 5.4 TB/s; two heads a thread, which read the tables once, 26.2, four 29.3: fewer threads with loads in flight.)
+template <typename T, bool INTER, bool VEC>
 __global__ __launch_bounds__(256) void rope_apply_kernel(const T* x, tc_strides xs, const float* __restrict__ c, const float* __restrict__ s,
-                                                         T* y, tc_strides ys, long long tokens, int rows, int heads, int groups, int items,
-                                                         int r, float sign) {
-  const RopeThread me = rope_thread(items, groups);
+                                                         T* y, tc_strides ys, long long tokens, int rows, int heads, int items, int r,
+                                                         float sign) {
+  const RopeThread me = rope_thread(items, heads);
   if (me.token >= tokens) return;
   const long long b = me.token / rows, t = me.token % rows;
   typedef RopeItem<T, INTER, VEC> Item;
   const Item it(c + me.token * (r / 2), s + me.token * (r / 2), me.item, r, sign);
-  const T* xr = x + b * xs.batch + t * xs.row;
-  T* yr = y + b * ys.batch + t * ys.row;
-  typename Item::Data v[PER];
-#pragma unroll
-  for (int k = 0; k < PER; k++) {
-    const int h = me.head + k * groups;
-    if (h < heads) it.load(xr + h * xs.head, v[k]);
-  }
-#pragma unroll
-  for (int k = 0; k < PER; k++) {
-    const int h = me.head + k * groups;
-    if (h < heads) {
-      it.turn(v[k]);
-      it.store(yr + h * ys.head, v[k]);
-    }
-  }
-}
-
-// Heads of a thread: four where the threads still fill the chip (256 compute units of 1024 threads).
-inline int rope_per(long long tokens, int heads, int items) {
-  return tokens * ((heads + 3) / 4) * items >= 256 * 1024 ? 4 : 1;
+  typename Item::Data v;
+  it.load(x + b * xs.batch + t * xs.row + me.head * xs.head, v);
+  it.turn(v);
+  it.store(y + b * ys.batch + t * ys.row + me.head * ys.head, v);
 }
 
 template <typename T, bool INTER, bool VEC>
 static int rope_launch(const tc_rope* p, int batch, int heads, int rows, const void* x, const tc_strides* xs, const float* c, const float* s,
                        void* y, const tc_strides* ys, int transposed, hipStream_t st) {
   const int r = rope_dim(p), items = rope_items(p->head_dim, r, Vec16<T>::N, INTER, VEC);
-  const long long tokens = (long long)batch * rows;
-  const int per = rope_per(tokens, heads, items), groups = (heads + per - 1) / per;
-  const long long blocks = (tokens * groups * items + 255) / 256;
+  const long long tokens = (long long)batch * rows, blocks = (tokens * heads * items + 255) / 256;
   if (blocks > 0x7fffffffLL) return TC_ERR_SHAPE;
-  const float sign = transposed ? -1.f : 1.f;
-#define TC_APPLY(PER_)                                                                                                                  \
-  rope_apply_kernel<T, INTER, VEC, PER_><<<(unsigned)blocks, 256, 0, st>>>((const T*)x, *xs, c, s, (T*)y, *ys, tokens, rows, heads, groups, \
-                                                                           items, r, sign)
-  if (per == 4)
-    TC_APPLY(4);
-  else
-    TC_APPLY(1);
-#undef TC_APPLY
+  rope_apply_kernel<T, INTER, VEC><<<(unsigned)blocks, 256, 0, st>>>((const T*)x, *xs, c, s, (T*)y, *ys, tokens, rows, heads, items, r,
+                                                                     transposed ? -1.f : 1.f);
   return check_launch();
 }
 
 // New tokens of a cache: the heads of a token are those of its query, key and value in turn.  Queries and keys are turned, queries go to
 // the rows of the output, keys and values to their slots.
-template <typename T, bool INTER, bool VEC, int PER>
+template <typename T, bool INTER, bool VEC>
 __global__ __launch_bounds__(256) void append_kernel(const T* __restrict__ Q, tc_strides qs, const T* __restrict__ K, tc_strides ks,
                                                      const T* __restrict__ V, tc_strides vs, const float* __restrict__ c,
                                                      const float* __restrict__ s, const int32_t* __restrict__ pos,
                                                      const int32_t* __restrict__ len, const int32_t* __restrict__ q_len, T* __restrict__ Qo,
                                                      T* __restrict__ Kc, T* __restrict__ Vc, int32_t* __restrict__ slot_pos,
-                                                     float* __restrict__ weight, CachePlan pl, int groups, int items, int r) {
-  const RopeThread me = rope_thread(items, groups);
+                                                     float* __restrict__ weight, CachePlan pl, int items, int r) {
+  const int heads = pl.H + 2 * pl.Hk;
+  const RopeThread me = rope_thread(items, heads);
   if (me.token >= (long long)pl.B * pl.T) return;
-  const int b = (int)(me.token / pl.T), t = (int)(me.token % pl.T);
+  const int b = (int)(me.token / pl.T), t = (int)(me.token % pl.T), h = me.head;
   typedef RopeItem<T, INTER, VEC> Item;
   // (without tables nothing is turned: the item's own part of the row is copied)
-  const Item it(c + (c ? me.token * (r / 2) : 0), s + (s ? me.token * (r / 2) : 0), me.item, r, 1.f);
+  const Item it(c ? c + me.token * (r / 2) : c, s ? s + me.token * (r / 2) : s, me.item, r, 1.f);
   const int m = q_len ? clamp_len(q_len[b], pl.T) : pl.T, slot = clamp_len(len[b], pl.max_len) - m + t;
-  const bool live = t < m, stored = live && slot >= 0 && slot < pl.cap;
-  const T* from[PER];
-  T* to[PER];
-  typename Item::Data v[PER];
-#pragma unroll
-  for (int k = 0; k < PER; k++) {
-    const int h = me.head + k * groups;
-    from[k] = nullptr;
-    to[k] = nullptr;
-    if (h < pl.H) {
-      to[k] = Qo + (((size_t)b * pl.H + h) * pl.T + t) * pl.dh;
-      if (live) from[k] = Q + b * qs.batch + h * qs.head + t * qs.row;
-    } else if (h < pl.H + 2 * pl.Hk && stored) {
-      const bool key = h < pl.H + pl.Hk;
-      const int j = h - (key ? pl.H : pl.H + pl.Hk);
-      const tc_strides& st = key ? ks : vs;
-      from[k] = (key ? K : V) + b * st.batch + j * st.head + t * st.row;
-      const size_t at = ((size_t)b * pl.Hk + j) * pl.cap + slot;
-      to[k] = (key ? Kc : Vc) + at * pl.dh;
-      if (key && me.item == 0) {
-        slot_pos[at] = pos[me.token];
-        weight[at] = 0.f;
-      }
+  const bool live = t < m;
+  typename Item::Data v;
+  if (h < pl.H) {
+    if (live) {
+      it.load(Q + b * qs.batch + h * qs.head + t * qs.row, v);
+      if (c) it.turn(v);
+    } else {
+      v.a = v.b = uint4{0, 0, 0, 0};
     }
-    if (from[k]) it.load(from[k], v[k]);
+    it.store(Qo + (((size_t)b * pl.H + h) * pl.T + t) * pl.dh, v);
+    return;
   }
-#pragma unroll
-  for (int k = 0; k < PER; k++) {
-    if (!to[k]) continue;
-    if (!from[k])
-      v[k].a = v[k].b = uint4{0, 0, 0, 0};
-    else if (c && me.head + k * groups < pl.H + pl.Hk)
-      it.turn(v[k]);
-    it.store(to[k], v[k]);
+  if (!live || slot < 0 || slot >= pl.cap) return;
+  const bool key = h < pl.H + pl.Hk;
+  const int j = h - (key ? pl.H : pl.H + pl.Hk);
+  const tc_strides& st = key ? ks : vs;
+  const size_t at = ((size_t)b * pl.Hk + j) * pl.cap + slot;
+  it.load((key ? K : V) + b * st.batch + j * st.head + t * st.row, v);
+  if (key && c) it.turn(v);
+  it.store((key ? Kc : Vc) + at * pl.dh, v);
+  if (key && me.item == 0) {
+    slot_pos[at] = pos[me.token];
+    weight[at] = 0.f;
   }
 }
 
@@ -269,18 +234,10 @@ static int append_launch(const CachePlan& pl, int r, const void* Q, const tc_str
                          const tc_strides* vs, const float* c, const float* s, const int32_t* pos, const int32_t* len, const int32_t* q_len,
                          void* Qo, void* Kc, void* Vc, int32_t* slot_pos, float* weight, hipStream_t st) {
   const int heads = pl.H + 2 * pl.Hk, items = rope_items(pl.dh, r, Vec16<T>::N, INTER, VEC);
-  const long long tokens = (long long)pl.B * pl.T;
-  const int per = rope_per(tokens, heads, items), groups = (heads + per - 1) / per;
-  const long long blocks = (tokens * groups * items + 255) / 256;
+  const long long blocks = ((long long)pl.B * pl.T * heads * items + 255) / 256;
   if (blocks > 0x7fffffffLL) return TC_ERR_SHAPE;
-#define TC_APPEND(PER_)                                                                                                                   \
-  append_kernel<T, INTER, VEC, PER_><<<(unsigned)blocks, 256, 0, st>>>((const T*)Q, *qs, (const T*)K, *ks, (const T*)V, *vs, c, s, pos, len, \
-                                                                       q_len, (T*)Qo, (T*)Kc, (T*)Vc, slot_pos, weight, pl, groups, items, r)
-  if (per == 4)
-    TC_APPEND(4);
-  else
-    TC_APPEND(1);
-#undef TC_APPEND
+  append_kernel<T, INTER, VEC><<<(unsigned)blocks, 256, 0, st>>>((const T*)Q, *qs, (const T*)K, *ks, (const T*)V, *vs, c, s, pos, len, q_len,
+                                                                 (T*)Qo, (T*)Kc, (T*)Vc, slot_pos, weight, pl, items, r);
   return check_launch();
 }
 

@@ -75,7 +75,7 @@ def test_heads(H, Hk):
     _run("f16", 128, 128, False, 2, H, Hk, 3, 20, [20, 11], None, seed=H)
 
 
-def test_many_tokens_take_several_heads_a_thread():
+def test_many_tokens_of_an_odd_number_of_heads():
     _run("bf16", 128, 128, False, 8, 33, 3, 200, 256, [256, 200, 230, 201, 255, 240, 210, 220], [200, 1, 100, 199, 7, 200, 150, 0])
 
 

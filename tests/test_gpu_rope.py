@@ -96,7 +96,7 @@ def test_rows_of_every_type_layout_and_share(dtype, inter, d, rot):
         assert torch.equal(wide, before)
 
 
-def test_large_rows_take_several_heads_a_thread():
+def test_many_rows_of_an_odd_number_of_heads():
     tc, orc = _tc()
     r, c, s, x, wide, want = _case(tc, orc, torch.bfloat16, 128, 128, False, 4, 33, 300, 3, False, "token")
     y = torch.empty(4, 33, 300, 128, dtype=torch.bfloat16, device="cuda")
