@@ -379,7 +379,8 @@ typedef struct {
   int32_t n_recent;     /* ... and the latest n_recent positions; n_sink, n_recent >= 0, n_sink + n_recent <= budget */
 } tc_cache;
 
-/* Bytes of scratch that any entry point may need for `c` (0 if c is invalid), whatever max_len is.  budget is looked at only by
+/* Bytes of scratch that any entry point may need for `c` (0 if c is invalid), whatever max_len is.  Where H/H_kv * T <= 16 there are 4 bytes
+   for each query row and slot among them (scores that tc_cache_attention keeps for the weights).  budget is looked at only by
    tc_cache_evict: 0 will do elsewhere. */
 TC_API size_t tc_cache_workspace_bytes(const tc_cache* c);
 
@@ -404,11 +405,14 @@ TC_API int tc_cache_append(const tc_cache* c, const tc_rope* r, const void* Q, c
  *     O[b, t, h*d_h + e] = sum_k p_k V_k[e],  p = softmax over the keys that the row sees of Q K^T * scale, rounded once
  *     weight[b, h_kv, j] += sum over the rows t < q_len[b] of the heads that share h_kv of p_j       (slots, not the prefix)
  *   Q         [B, H, T, d_h]            (Q_out of tc_cache_append)
- *   K_prefix, V_prefix [n_prefixes, H_kv, P, d_h]  both NULL where P = 0.  A prefix is read once for all rows of its sequences
+ *   K_prefix, V_prefix [n_prefixes, H_kv, P, d_h]  both NULL where P = 0.  Where H/H_kv * T <= 16 a prefix is read once for
+ *             all its sequences (if that spares 32 MB and more), else once for the rows of each
  *   K_cache, V_cache [B, H_kv, capacity, d_h]      slots behind len[b] are not looked at: they may hold anything
  *   O         [B, T, H*d_h]             rows t >= q_len[b], and rows that see no key, are zero
  *   weight    [B, H_kv, capacity] float, read and written, sums in a fixed order; NULL: not wanted
- * What a row does not see has no influence on it, infinities and NaN included.  No two tensors overlap.
+ * What a row does not see has no influence on it, infinities and NaN included.  No two tensors overlap.  16-bit storage: probabilities enter
+ * their products as a 16-bit head and remainder in tiles of up to 16 rows, rounded to 16 bits in larger ones (an error of the size of O's own
+ * rounding).
  */
 TC_API int tc_cache_attention(const tc_cache* c, const void* Q, const void* K_prefix, const void* V_prefix, const void* K_cache,
                               const void* V_cache, const int32_t* len, const int32_t* q_len, void* O, float* weight, void* ws,

@@ -1120,8 +1120,11 @@ template <typename T, int DH>
 static int attention_launch(const CachePlan& pl, AttnArgs a, hipStream_t st) {
   const Cut cut = make_cut(pl, pl.max_len);
   a.parts = cut.parts;
-  long long chunks = (pl.max_len + GK - 1) / GK;
-  if (workgroups(cut.job[0]) + workgroups(cut.job[1]) > 0x7fffffffLL || (a.weight && chunks * pl.B * pl.Hk > 0x7fffffffLL)) return TC_ERR_SHAPE;
+  const int row_wgs = join_workgroups(a);
+  // slots of a workgroup that gathers: from the scores that were kept, where parts are joined, or by scores formed anew
+  const int per = a.score ? GW : GK;
+  const long long chunks = ((long long)pl.max_len + per - 1) / per, gather_wgs = a.weight ? chunks * pl.B * pl.Hk : 0;
+  if (workgroups(cut.job[0]) + workgroups(cut.job[1]) > 0x7fffffffLL || row_wgs + gather_wgs > 0x7fffffffLL) return TC_ERR_SHAPE;
   Job few[2] = {};
   int nf = 0;
   for (int k = 0; k < cut.jobs; k++) {
@@ -1143,24 +1146,18 @@ static int attention_launch(const CachePlan& pl, AttnArgs a, hipStream_t st) {
     if (!allow_lds(kernel, waves * F::WAVE)) return TC_ERR_HIP;
     kernel<<<(unsigned)(workgroups(few[0]) + workgroups(few[1])), 64 * waves, waves * F::WAVE, st>>>(a, few[0], few[1]);
   }
-  const int row_wgs = join_workgroups(a);
-  if (a.weight && a.score) {
-    if (a.parts == 1) return check_launch();  // done by few_kernel
-    chunks = (pl.max_len + GW - 1) / GW;
-    const long long wgs = row_wgs + chunks * pl.B * pl.Hk;
-    if (wgs > 0x7fffffffLL) return TC_ERR_SHAPE;
-    join_gather_kernel<T, DH><<<(unsigned)wgs, 256, 0, st>>>(a, row_wgs, Div((uint32_t)chunks));
-    return check_launch();
+  if (a.score) {
+    if (a.parts > 1) join_gather_kernel<T, DH><<<(unsigned)(row_wgs + gather_wgs), 256, 0, st>>>(a, row_wgs, Div((uint32_t)chunks));
+    return check_launch();  // (a single part: few_kernel has gathered)
   }
   if (a.parts > 1) join_kernel<T, DH><<<row_wgs, 256, 0, st>>>(a);
   if (a.weight) {
-    const unsigned wgs = (unsigned)(chunks * pl.B * pl.Hk);
     bool done = false;
     if constexpr (sizeof(T) == 2) {
       done = pl.R > GATHER_ROWS;
-      if (done) gather_many_kernel<T, DH><<<wgs, 256, 0, st>>>(a, Div((uint32_t)chunks));
+      if (done) gather_many_kernel<T, DH><<<(unsigned)gather_wgs, 256, 0, st>>>(a, Div((uint32_t)chunks));
     }
-    if (!done) gather_kernel<T, DH><<<wgs, 256, 0, st>>>(a, Div((uint32_t)chunks));
+    if (!done) gather_kernel<T, DH><<<(unsigned)gather_wgs, 256, 0, st>>>(a, Div((uint32_t)chunks));
   }
   return check_launch();
 }

@@ -290,6 +290,8 @@ extern "C" int tc_cache_evict(const tc_cache* c, const int32_t* len, const void*
   EvictArgs a = {len, slot_pos, weight, source, list, len_out, pl.Hk, pl.cap, pl.max_len, pl.budget, pl.sink, pl.recent, (uint4*)K_out, (uint4*)V_out,
                  pos_out, weight_out, vecs};
   const bool fused = same == 4 && pl.max_len - pl.budget <= EV_FUSED;
+  const int rows = 256 / vecs, most = pl.max_len < pl.budget ? pl.max_len : pl.budget, chunks = (most + rows - 1) / rows;
+  if (!fused && (long long)heads * chunks > 0x7fffffffLL) return TC_ERR_SHAPE;
 #define TC_EVICT(NT_, KPT_)                                        \
   do {                                                             \
     if (fused)                                                     \
@@ -307,8 +309,6 @@ extern "C" int tc_cache_evict(const tc_cache* c, const int32_t* len, const void*
     TC_EVICT(1024, 0);
 #undef TC_EVICT
   if (fused) return check_launch();
-  const int rows = 256 / vecs, most = pl.max_len < pl.budget ? pl.max_len : pl.budget, chunks = (most + rows - 1) / rows;
-  if ((long long)heads * chunks > 0x7fffffffLL) return TC_ERR_SHAPE;
   evict_move_kernel<<<heads * chunks, 256, 0, st>>>(len, source, (const uint4*)K_cache, (const uint4*)V_cache, slot_pos, weight, (uint4*)K_out,
                                                     (uint4*)V_out, pos_out, weight_out, pl.Hk, pl.cap, out_capacity, pl.max_len, pl.budget, vecs,
                                                     chunks, same == 4);

@@ -84,6 +84,28 @@ def test_without_tables_rows_are_copied(dtype):
     _run(dtype, 64, 64, False, 2, 3, 1, 4, 12, [12, 7], [4, 3], turned=False)
 
 
+def test_the_largest_number_of_sequences_and_rows():
+    tc, orc = _tc()
+    for B, T in ((65536, 1), (1, 1 << 20)):
+        q = torch.randn(B, 1, T, 64, device="cuda").bfloat16()
+        c = tc.make_cache(B, 1, 1, 64, tc.TC_BF16, T, T + 1)
+        pos = torch.arange(B * T, dtype=torch.int32, device="cuda").view(B, T)
+        K, V = torch.zeros(B, 1, T + 1, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(B, 1, T + 1, 64, dtype=torch.bfloat16, device="cuda")
+        sp, w = torch.full((B, 1, T + 1), -1, dtype=torch.int32, device="cuda"), torch.ones(B, 1, T + 1, device="cuda")
+        lens, out = torch.full((B,), T + 1, dtype=torch.int32, device="cuda"), torch.empty_like(q)
+        r, co, si = tc.make_rope(64), torch.empty(B, T, 32, device="cuda"), torch.empty(B, T, 32, device="cuda")
+        tc.tc_rope_tables(r, pos, co, si)
+        tc.tc_cache_append(c, r, q, q, q, co, si, pos, lens, out, K, V, sp, w)
+        want = torch.empty_like(q)
+        tc.tc_rope_apply(r, q, co, si, want)
+        assert torch.equal(out, want) and torch.equal(K[:, :, 1:], want) and torch.equal(V[:, :, 1:], q) and not K[:, :, 0].any()
+        assert torch.equal(sp[:, 0, 1:], pos) and not w[:, :, 1:].any() and (w[:, :, 0] == 1).all() and (sp[:, :, 0] == -1).all()
+        i = B * T - 1
+        wc, ws = orc.rope_tables(np.array([i]), orc.rope_theta(64))
+        row = orc.rope_apply(q.view(-1, 64)[i].double().cpu().numpy()[None], wc, ws)
+        assert _near(out.view(-1, 64)[i][None], row, torch.bfloat16)
+
+
 def test_refusals():
     tc, _ = _tc()
     c = tc.make_cache(1, 2, 1, 64, tc.TC_BF16, 2, 8)

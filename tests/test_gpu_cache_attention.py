@@ -223,6 +223,30 @@ def test_offsets_beyond_32_bits():
     assert (O[-1].float() - s["O"][0].float()).abs().max() <= 2.0 ** -7 * s["O"].float().abs().max() and not O[:-1].any()
 
 
+def test_the_largest_numbers_of_sequences_rows_and_heads():
+    tc, _ = _tc()
+    new = lambda *s, dtype=torch.bfloat16: torch.randn(*s, device="cuda").to(dtype)  # noqa: E731
+    for B, H, Hk, T, cap in ((65536, 1, 1, 1, 3), (1, 1, 1, 1 << 20, 40), (2, 1024, 1, 1, 70), (2, 1024, 1024, 1, 5)):
+        c = tc.make_cache(B, H, Hk, 64, tc.TC_BF16, T, cap, budget=2)
+        Q, K, V = new(B, H, T, 64), new(B, Hk, cap, 64), new(B, Hk, cap, 64)
+        lens, q_len = torch.full((B,), cap, dtype=torch.int32, device="cuda"), torch.full((B,), min(T, 2), dtype=torch.int32, device="cuda")
+        O, w, ws = torch.empty(B, T, H * 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(B, Hk, cap, device="cuda"), tc.new_cache_workspace(c)
+        tc.tc_cache_attention(c, Q, K, V, lens, O, ws, weight=w, q_len=q_len)
+        m = min(T, 2)
+        x = (Q[:, :, :m].double().view(B, Hk, -1, 64) @ K.double().transpose(2, 3).contiguous()) / 8
+        if m == 2:
+            x[:, :, 0, cap - 1] = -float("inf")   # (one head) the first of two rows does not see the last slot
+        p = x.softmax(-1)
+        want = (p @ V.double()).view(B, H, m, 64).transpose(1, 2).reshape(B, m, H * 64)
+        # one rounding of the output and one of the probabilities, of values of at most 5.6
+        assert (O[:, :m].double() - want).abs().max() <= 2 * 2.0 ** -8 * 5.6 and not O[:, m:].any()
+        assert (w.double() - p.sum(2)).abs().max() <= 2.0 ** -16 * p.sum(2).max()
+        sp, left = torch.arange(cap, dtype=torch.int32, device="cuda").repeat(B, Hk, 1), torch.empty(B, dtype=torch.int32, device="cuda")
+        tc.tc_cache_evict(c, lens, K, V, sp, w, left, ws)
+        best = p.sum(2).topk(2, dim=-1).values.sum(-1)
+        assert (w[:, :, :2].double().sum(-1) - best).abs().max() <= 2.0 ** -15 * best.max() and (left == 2).all()
+
+
 def test_refusals():
     tc, _ = _tc()
     s = make("bf16", 64, 2, 4, 2, 3, 20, [20, 9], [3, 1], images=1, P=7)
