@@ -136,7 +136,8 @@ struct AttnArgs {
   int rows;     // all rows: B H T
   int parts;    // parts of the keys of a row
   float scale2; // scale log2(e)
-  float offset; // probabilities are formed as 2^(s - m - offset), so that sums of them times values stay within float32
+  float offset; // probabilities are formed as 2^(s - m - offset): for exponents of float32 so that sums of them times values stay within float32; half:
+                // as large as the type holds, which sets the small ones apart from 0 (65536 keys of 2^-26 of the largest are a thousandth)
 };
 
 // A share of a call: the rows of a group against the keys of a prefix, of the group's cache, or both.  A group is what has one
@@ -608,6 +609,7 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
   typedef ManyShape<DH> S;
   typedef ManyWave<T, DH, KW> Wave;
   constexpr int ROWS = MROWS / KW, RW = 4 / KW;  // rows of the workgroup, wavefronts that share them
+  const float offset = a.offset + LAZY;          // (a probability may pass that of the running maximum so far)
   extern __shared__ __attribute__((aligned(16))) unsigned char cache_smem[];
   __shared__ int flag[3];
   __shared__ size_t places[4][32];  // of rows in the output
@@ -697,7 +699,7 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
     const unsigned char* Ks = cache_smem + (t & 1) * S::STAGE;
     if (!idle && k0 < (pre ? a.P : wave_most)) {
       const bool masked = k0 + MK / KW > (pre ? a.P : wave_least);
-      w.step(Ks + ku * S::KLD, Ks + MK * S::KLD + ku * S::VLD, k0, lim, masked, a.scale2, a.offset, lane);
+      w.step(Ks + ku * S::KLD, Ks + MK * S::KLD + ku * S::VLD, k0, lim, masked, a.scale2, offset, lane);
       if (masked && __builtin_amdgcn_readfirstlane(flag[t % 3]))
         w.add_odd(static_cast<const T*>(pre ? a.Vp : a.Vc) + ((pre ? phead : head) + k0) * DH, min(MK / KW, (pre ? a.P : most) - k0), lim - k0, lane);
     }
@@ -733,7 +735,7 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
   if (a.parts > 1) {
     if (!mine) return;
     const size_t at = (size_t)(job.part0 + split) * a.rows + row;
-    if (half == 0) a.ml[at] = f2{w.mx == -INFINITY ? w.mx : w.mx + a.offset, total};
+    if (half == 0) a.ml[at] = f2{w.mx == -INFINITY ? w.mx : w.mx + offset, total};
     if (t0 >= t1) return;
 #pragma unroll
     for (int d = 0; d < DH / 32; d++)
@@ -743,7 +745,7 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
     return;
   }
   if (idle) return;
-  if (a.lse && half == 0 && mine) a.lse[row] = live ? (w.mx == -INFINITY ? 0.f : w.mx) + a.offset + log2f(total) : INFINITY;
+  if (a.lse && half == 0 && mine) a.lse[row] = live ? (w.mx == -INFINITY ? 0.f : w.mx) + offset + log2f(total) : INFINITY;
   const bool sees = live && a.P + end > 0;
   const float inv = 1.f / total;
   unsigned char* Os = cache_smem + 2 * 64 * (DH / 2 + 2) * 4 * (KW - 1) + wave * 32 * S::KLD;
@@ -1186,7 +1188,7 @@ extern "C" int tc_cache_attention(const tc_cache* c, const void* Q, const void* 
   a.scale2 = pl.scale * 1.44269504088896340736f;
   int bits = 1;  // 2^bits is more than twice the keys of a row
   while ((1LL << bits) <= 2LL * pl.P + 2LL * pl.max_len) bits++;
-  a.offset = c->dtype == TC_F16 ? 0.f : bits + LAZY;  // (half: its values times float32 sums are far from that range, and small halves lose bits)
+  a.offset = c->dtype == TC_F16 ? -15.f : (float)bits;  // (half: its values times sums of 2^15 are far from the range of float32)
   char* w = static_cast<char*>(ws);
   a.lse = weight ? reinterpret_cast<float*>(w) : nullptr;
   w += align256((size_t)a.rows * 4);

@@ -191,6 +191,25 @@ def test_peaked_and_scaled_scores(dtype):
     check(make(dtype, 64, 2, 2, 2, 33, 200, [200, 111], scale=1e-3, images=1, P=64))
 
 
+@pytest.mark.parametrize("T", [1, 16, 40, 80])
+def test_many_halves_far_below_the_largest(T):
+    """One key has all but a thousandth of the attention, 40000 others 2^-25.4 of its each: rounded to halves as they are they would be nothing.
+    They are rounded as multiples of 2^-24 after a factor: 2^15 in small tiles, whose remainder is exact to half a step, 2^-40 of the largest;
+    2^7 at least in large ones, 2^-32."""
+    _, orc = _tc()
+    n = 40000
+    s = make("f16", 64, 1, 1, 1, T, n, [n])
+    s["Q"].zero_(), s["K"].zero_()
+    s["Q"][..., 0], s["K"][0, 0, 0, 0], s["V"][0, 0, 0], s["V"][0, 0, 1:] = 16.0, 8.8, 0.0, 1.0
+    call(s)
+    want, _ = orc.attention(*(s[k][0].cpu().double().numpy() for k in ("Q", "K", "V")), n, T)
+    got = s["O"][0].cpu().double().numpy()
+    want = np.asarray(want).reshape(T, 64)
+    h, rel = 2.0 ** -11, 2 * (2.0 ** -24 * 68 * 17.6 + 2.0 ** -20)
+    bound = (h + (h if T > 16 else h * h) + rel) * want + n * (2.0 ** -32 if T > 16 else 2.0 ** -40)
+    assert 8e-4 < want.min() and np.all(np.abs(got - want) <= bound), np.max(np.abs(got - want) / want)
+
+
 def test_weights_gather_over_calls_and_are_the_same_each_time():
     s = make("bf16", 128, 3, 8, 2, 1, 700, [700, 650, 9], images=1, P=128)
     start = s["w"].clone()
