@@ -306,8 +306,9 @@ TC_API int tc_probe_rates(void* ws, size_t ws_bytes, void* stream, float* rates)
 /* ---- behind the compression: rotary positions and the cache of keys and values -------------------------------------------
  *
  * What the layers behind the compression do with the shortened sequence and with the tokens that follow it.  The conventions
- * above hold, with two additions: rows that carry strides (tc_strides) may be views, and lengths per sequence are device
- * arrays, which are clamped where they are out of range, not reported.
+ * above hold, with three additions: rows that carry strides (tc_strides) may be views; lengths per sequence are device
+ * arrays, which are clamped where they are out of range, not reported; what a launch cannot hold (2^32 threads, so some 2^24 heads of
+ * sequences) is refused with TC_ERR_SHAPE before anything is launched.
  */
 typedef enum { TC_ROPE_HALF = 0, TC_ROPE_INTERLEAVED = 1 } tc_rope_layout;
 /* the angle per position of pair i, theta_i = base^(-2 i / r), for contexts longer than the model was trained on:

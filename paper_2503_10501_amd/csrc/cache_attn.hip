@@ -1126,7 +1126,7 @@ static int attention_launch(const CachePlan& pl, AttnArgs a, hipStream_t st) {
   // slots of a workgroup that gathers: from the scores that were kept, where parts are joined, or by scores formed anew
   const int per = a.score ? GW : GK;
   const long long chunks = ((long long)pl.max_len + per - 1) / per, gather_wgs = a.weight ? chunks * pl.B * pl.Hk : 0;
-  if (workgroups(cut.job[0]) + workgroups(cut.job[1]) > 0x7fffffffLL || row_wgs + gather_wgs > 0x7fffffffLL) return TC_ERR_SHAPE;
+  if (!grid_fits(workgroups(cut.job[0]) + workgroups(cut.job[1]), cut.job[0].wide ? 512 : 256) || !grid_fits(row_wgs + gather_wgs, 256)) return TC_ERR_SHAPE;
   Job few[2] = {};
   int nf = 0;
   for (int k = 0; k < cut.jobs; k++) {

@@ -68,6 +68,9 @@ inline int check_cache_ws(const CachePlan& pl, const void* ws, size_t ws_bytes) 
   return ws_bytes < pl.total ? TC_ERR_WORKSPACE : TC_OK;
 }
 
+// Workgroups of a launch and their threads: a grid counts its threads in 32 bits.
+inline bool grid_fits(long long workgroups, int threads) { return workgroups * threads < (1LL << 32); }
+
 __device__ inline int clamp_len(int n, int most) { return n < 0 ? 0 : (n > most ? most : n); }
 
 }  // namespace tc

@@ -291,7 +291,8 @@ extern "C" int tc_cache_evict(const tc_cache* c, const int32_t* len, const void*
                  pos_out, weight_out, vecs};
   const bool fused = same == 4 && pl.max_len - pl.budget <= EV_FUSED;
   const int rows = 256 / vecs, most = pl.max_len < pl.budget ? pl.max_len : pl.budget, chunks = (most + rows - 1) / rows;
-  if (!fused && (long long)heads * chunks > 0x7fffffffLL) return TC_ERR_SHAPE;
+  const int threads = pl.max_len <= EV_SMALL ? 256 : pl.max_len <= EV_MIDDLE ? 512 : 1024;
+  if (!grid_fits(heads, threads) || (!fused && !grid_fits((long long)heads * chunks, 256))) return TC_ERR_SHAPE;
 #define TC_EVICT(NT_, KPT_)                                        \
   do {                                                             \
     if (fused)                                                     \

@@ -180,7 +180,7 @@ static int rope_launch(const tc_rope* p, int batch, int heads, int rows, const v
                        void* y, const tc_strides* ys, int transposed, hipStream_t st) {
   const int r = rope_dim(p), items = rope_items(p->head_dim, r, Vec16<T>::N, INTER, VEC);
   const long long tokens = (long long)batch * rows, blocks = (tokens * heads * items + 255) / 256;
-  if (blocks > 0x7fffffffLL) return TC_ERR_SHAPE;
+  if (!grid_fits(blocks, 256)) return TC_ERR_SHAPE;
   rope_apply_kernel<T, INTER, VEC><<<(unsigned)blocks, 256, 0, st>>>((const T*)x, *xs, c, s, (T*)y, *ys, tokens, rows, heads, items, r,
                                                                      transposed ? -1.f : 1.f);
   return check_launch();
@@ -235,7 +235,7 @@ static int append_launch(const CachePlan& pl, int r, const void* Q, const tc_str
                          void* Qo, void* Kc, void* Vc, int32_t* slot_pos, float* weight, hipStream_t st) {
   const int heads = pl.H + 2 * pl.Hk, items = rope_items(pl.dh, r, Vec16<T>::N, INTER, VEC);
   const long long blocks = ((long long)pl.B * pl.T * heads * items + 255) / 256;
-  if (blocks > 0x7fffffffLL) return TC_ERR_SHAPE;
+  if (!grid_fits(blocks, 256)) return TC_ERR_SHAPE;
   append_kernel<T, INTER, VEC><<<(unsigned)blocks, 256, 0, st>>>((const T*)Q, *qs, (const T*)K, *ks, (const T*)V, *vs, c, s, pos, len, q_len,
                                                                  (T*)Qo, (T*)Kc, (T*)Vc, slot_pos, weight, pl, items, r);
   return check_launch();
@@ -270,7 +270,7 @@ extern "C" int tc_rope_tables(const tc_rope* r, const int32_t* pos_ids, int64_t 
   const int64_t blocks1 = (n + rows - 1) / rows;
   const int per = blocks1 >= 8 * 1024 ? 8 : blocks1 >= 2 * 1024 ? (int)(blocks1 / 1024) : 1;  // positions of a thread: its angle is worth keeping once the chip is full
   const int64_t blocks = (blocks1 + per - 1) / per;
-  if (blocks > 0x7fffffffLL) return TC_ERR_SHAPE;
+  if (!grid_fits(blocks, 256)) return TC_ERR_SHAPE;
   rope_tables_kernel<<<(unsigned)blocks, 256, 0, (hipStream_t)stream>>>(pos_ids, n, cos, sin, half, log_base, r->scaling, (double)r->factor,
                                                                         (double)r->original_len, (double)r->low, (double)r->high,
                                                                         r->magnitude > 0.f ? (double)r->magnitude : 1.0, per);

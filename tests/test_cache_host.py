@@ -149,6 +149,23 @@ def test_cache_entry_points_check_their_arguments():
 
 
 @needs_library
+def test_what_no_grid_holds_is_refused():
+    """A grid counts its threads in 32 bits."""
+    tc = _binding()
+    lib, F = tc.load_library(), FAKE
+    big = dict(batch=1 << 16, n_heads=1024, n_kv_heads=1024, head_dim=64, dtype=1, n_query=1, capacity=4)
+    for kw in (dict(big, budget=2), dict(big, budget=4, batch=1 << 15, n_heads=512, n_kv_heads=512)):
+        calls = _calls(tc, c=ctypes.byref(tc.make_cache(**kw)), Kp=None, Vp=None, bytes=1 << 60)
+        assert calls["attention"]() == calls["evict"]() == -2
+    c = tc.make_cache(**dict(big, batch=1, n_query=1 << 20))
+    assert _calls(tc, c=ctypes.byref(c))["append"]() == -2
+    st = ctypes.byref(tc.tc_strides(1 << 30, 128, 1 << 17))
+    r = ctypes.byref(tc.make_rope(128, rot_dim=2))
+    assert lib.tc_rope_apply(r, tc.TC_BF16, 1 << 8, 1024, 1 << 13, F, st, F, F, F, st, 0, None) == -2
+    assert lib.tc_rope_tables(r, F, 1 << 36, F, F, None) == -2
+
+
+@needs_library
 def test_cache_workspace_grows_with_the_cache_and_not_with_the_call():
     tc = _binding()
     size = lambda **kw: tc.tc_cache_workspace_bytes(tc.make_cache(**dict(CACHE, **kw)))  # noqa: E731
