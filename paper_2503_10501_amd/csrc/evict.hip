@@ -42,7 +42,8 @@ constexpr int EV_FUSED = 64;  // at most so many slots beyond the budget: the se
 // One workgroup per sequence and head.  The slots are dealt to the wavefronts in runs, a run's 64 lanes side by side, KPT keys of a lane in
 // registers (KPT = 0: any number of slots, the keys formed anew each time).  The threshold, the largest key that at least `budget` slots reach, is
 // found two bits at a time from counts of three candidates, until one is reached by `budget` slots exactly; equal keys stay from the lowest
-// slot on.  Then each freed place takes the survivor of its rank.
+// slot on.  Then each freed place takes the survivor of its rank.  A chain of at most 16 counts and barriers bounds it, not its bytes (8 for a slot):
+// 8 x 32 heads of up to 2944 slots 12.9 us; counts by atomics on a histogram in LDS took longer than a wavefront's ballots.
 template <int NT, int KPT, bool FUSED>
 __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
   constexpr int W = NT / 64, UN = KPT > 0 ? KPT : 1;
@@ -235,7 +236,7 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(EvictArgs a) {
 }
 
 // Rows to their places: a row's 16-byte vectors side by side, one of keys and one of values for a thread.  (8 x 32 heads, 640 rows of 256 bytes each out
-// of up to 2944: 28 us, 5.8 TB/s; two rows a thread 36, four 52: the loads of rows that may not move are not issued together.)
+// of up to 2944: 27 us, 5.8 TB/s; two rows a thread 36, four 52: the loads of rows that may not move are not issued together.)
 __global__ __launch_bounds__(256) void evict_move_kernel(const int32_t* __restrict__ len, const int32_t* __restrict__ source, const uint4* K,
                                                          const uint4* V, const int32_t* pos, const float* weight, uint4* Ko, uint4* Vo,
                                                          int32_t* po, float* wo, int Hk, int cap, int out_cap, int max_len, int budget,
