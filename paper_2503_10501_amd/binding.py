@@ -282,7 +282,7 @@ def tc_kv_cache_fraction(n_text, n_vis, n_kept, n_layers, n_layers_before):
 
 
 # ---- behind the compression: the tensors' shapes are checked, and work goes to the device that holds them.  A decoding step makes these
-# calls for every layer: they keep to what a check costs (15 tensors: 5 us).
+# calls for every layer: they keep to what a check costs (14 tensors: 5 us).
 
 _I32, _F32, _U8 = torch.int32, torch.float32, torch.uint8
 _STORAGE = {TC_F32: torch.float32, TC_BF16: torch.bfloat16, TC_F16: torch.float16}
