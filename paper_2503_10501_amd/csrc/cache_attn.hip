@@ -614,8 +614,10 @@ struct ManyWave {
   }
 };
 
-template <typename T, int DH, int KW>
-__global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
+// GATHER: the workgroup has all rows of its group and all of their keys, and adds what the slots gather itself, from scores formed again, with the keys
+// in the lanes and the rows in registers.
+template <typename T, int DH, int KW, bool GATHER>
+__global__ __launch_bounds__(256, KW == 2 && DH == 64 ? 4 : 2) void many_kernel(AttnArgs a, Job job) {
   typedef ManyShape<DH> S;
   typedef ManyWave<T, DH, KW> Wave;
   constexpr int ROWS = MROWS / KW, RW = 4 / KW;  // rows of the workgroup, wavefronts that share them
@@ -623,6 +625,12 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
   extern __shared__ __attribute__((aligned(16))) unsigned char cache_smem[];
   __shared__ int flag[3];
   __shared__ size_t places[4][32];  // of rows in the output
+  // where it gathers: behind the outputs, in the place of the tiles
+  constexpr int KEYS = 32 * Wave::NU, GBYTES = ROWS * 8 + 2 * 4 * KEYS * 4;
+  static_assert((KW - 1) * 2 * 64 * (DH / 2 + 2) * 4 + RW * 32 * S::KLD <= S::LDS - GBYTES && GBYTES % 16 == 0);
+  float* row_lse = reinterpret_cast<float*>(cache_smem + S::LDS - GBYTES);
+  int* row_end = reinterpret_cast<int*>(row_lse + ROWS);
+  float* sums = reinterpret_cast<float*>(row_end + ROWS);  // [2][wavefront][key]
   int group, item;
   if (!group_on_xcd(blockIdx.x, job.tiles * job.splits, job.groups, &group, &item)) return;
   const int back = job.by_splits.quot(item), split = item - back * job.splits, tile = job.tiles - 1 - back;  // (the rows that see the most first)
@@ -731,7 +739,7 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
         for (int e = 0; e < 16; e++) at[64 * (2 + 16 * d + e)] = w.o[d][e];
     }
     __syncthreads();
-    if (wave >= RW) return;
+    if (!GATHER && wave >= RW) return;
     const float mx = fmaxf(w.mx, at[0]), ref = mx == -INFINITY ? 0.f : mx;
     const float f0 = exp2_fast(w.mx - ref), f1 = exp2_fast(at[0] - ref);
     total = total * f0 + at[64] * f1;
@@ -754,25 +762,87 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttnArgs a, Job job) {
         *reinterpret_cast<f4*>(a.part + at * DH + 32 * d + 8 * e + 4 * half) = f4{w.o[d][4 * e], w.o[d][4 * e + 1], w.o[d][4 * e + 2], w.o[d][4 * e + 3]};
     return;
   }
-  if (idle) return;
-  if (a.lse && half == 0 && mine) a.lse[row] = live ? (w.mx == -INFINITY ? 0.f : w.mx) + offset + log2f(total) : INFINITY;
-  const bool sees = live && a.P + end > 0;
-  const float inv = 1.f / total;
-  unsigned char* Os = cache_smem + 2 * 64 * (DH / 2 + 2) * 4 * (KW - 1) + wave * 32 * S::KLD;
-  if (half == 0) places[wave][i] = out_row(a, b, hk * a.G + head_of, tok, DH);
+  if (!GATHER && idle) return;
+  const float lse = live ? (w.mx == -INFINITY ? 0.f : w.mx) + offset + log2f(total) : INFINITY;
+  // keys of the slots as operands, 32 of a wavefront's in each run: lane i has part of slot k0 + i
+  typename Mma<T>::frag ks[GATHER ? Wave::NU : 1][DH / 16];
+  auto load_slots = [&](int k0) {
 #pragma unroll
-  for (int d = 0; d < DH / 32; d++)
+    for (int u = 0; u < Wave::NU; u++) {
+      const u4* Kr = reinterpret_cast<const u4*>(static_cast<const T*>(a.Kc) + (head + min(k0 + ku + 32 * u + i, a.cap - 1)) * DH);
 #pragma unroll
-    for (int e = 0; e < 8; e++) {
-      const float y0 = sees ? w.o[d][2 * e] * inv : 0.f, y1 = sees ? w.o[d][2 * e + 1] * inv : 0.f;
-      *reinterpret_cast<uint32_t*>(Os + i * S::KLD + (32 * d + 8 * (e >> 1) + 4 * half + 2 * (e & 1)) * 2) = Mma<T>::head(y0, y1);
+      for (int c = 0; c < DH / 16; c++) ks[u][c].u = Kr[2 * c + half];
     }
-  wave_lds_order();
+  };
+  if constexpr (GATHER) {
+    load_slots(0);
+    if (half == 0 && (KW == 1 || wave < RW)) {
+      row_lse[wave % RW * 32 + i] = lse;
+      row_end[wave % RW * 32 + i] = live ? end : 0;
+    }
+  } else if (a.lse && half == 0 && mine) {
+    a.lse[row] = lse;
+  }
+  const bool sees = live && a.P + end > 0;
+  if (!GATHER || (!idle && wave % RW == wave)) {
+    const float inv = 1.f / total;
+    unsigned char* Os = cache_smem + 2 * 64 * (DH / 2 + 2) * 4 * (KW - 1) + wave * 32 * S::KLD;
+    if (half == 0) places[wave][i] = out_row(a, b, hk * a.G + head_of, tok, DH);
 #pragma unroll
-  for (int j = 0; j < 32 * S::VEC / 64; j++) {
-    const int at = lane + 64 * j, rr = at / S::VEC, c = at % S::VEC;
-    if (r0 + rr >= 0)
-      *reinterpret_cast<u4*>(static_cast<T*>(a.O) + places[wave][rr] + 8 * c) = *reinterpret_cast<const u4*>(Os + rr * S::KLD + c * 16);
+    for (int d = 0; d < DH / 32; d++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const float y0 = sees ? w.o[d][2 * e] * inv : 0.f, y1 = sees ? w.o[d][2 * e + 1] * inv : 0.f;
+        *reinterpret_cast<uint32_t*>(Os + i * S::KLD + (32 * d + 8 * (e >> 1) + 4 * half + 2 * (e & 1)) * 2) = Mma<T>::head(y0, y1);
+      }
+    wave_lds_order();
+#pragma unroll
+    for (int j = 0; j < 32 * S::VEC / 64; j++) {
+      const int at = lane + 64 * j, rr = at / S::VEC, c = at % S::VEC;
+      if (r0 + rr >= 0)
+        *reinterpret_cast<u4*>(static_cast<T*>(a.O) + places[wave][rr] + 8 * c) = *reinterpret_cast<const u4*>(Os + rr * S::KLD + c * 16);
+    }
+  }
+  if constexpr (GATHER) {
+    __syncthreads();
+    // element e of a product is that of row 8 (e / 4) + 4 half + e % 4 and the lane's key
+    float rl[16];
+    int re[16];
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+      const int at = wave % RW * 32 + 8 * e + 4 * half;
+      *reinterpret_cast<f4*>(rl + 4 * e) = *reinterpret_cast<const f4*>(row_lse + at);
+      *reinterpret_cast<u4*>(re + 4 * e) = *reinterpret_cast<const u4*>(row_end + at);
+    }
+    if (m == 0) most = 0;
+    for (int k0 = 0; k0 < most; k0 += MK) {
+      float* now = sums + (k0 / MK & 1) * 4 * KEYS;  // (the other one is still being read)
+#pragma unroll
+      for (int u = 0; u < Wave::NU; u++) {
+        const int key = k0 + ku + 32 * u + i;
+        f16v s;
+#pragma unroll
+        for (int e = 0; e < 16; e++) s[e] = 0.f;
+#pragma unroll
+        for (int c = 0; c < DH / 16; c++) s = Mma<T>::mul32(w.q[c], ks[u][c], s);
+        float acc = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; e++) {
+          const float p = exp2_fast(fmaf(s[e], a.scale2, -rl[e]));
+          acc += key < re[e] ? p : 0.f;
+        }
+        const u2 y = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc), __float_as_uint(acc), false, false);
+        if (half == 0) now[wave * KEYS + 32 * u + i] = __uint_as_float(y[0]) + __uint_as_float(y[1]);
+      }
+      if (k0 + MK < most) load_slots(k0 + MK);
+      __syncthreads();
+      if (tid < MK && k0 + tid < most) {
+        float all = 0.f;
+#pragma unroll
+        for (int x = 0; x < RW; x++) all += now[(tid / KEYS * RW + x) * KEYS + tid % KEYS];
+        a.weight[head + k0 + tid] += all;
+      }
+    }
   }
 }
 
@@ -1139,6 +1209,8 @@ static int attention_launch(const CachePlan& pl, AttnArgs a, hipStream_t st) {
   const int per = a.score ? GW : GK;
   const long long chunks = ((long long)pl.max_len + per - 1) / per, gather_wgs = a.weight ? chunks * pl.B * pl.Hk : 0;
   if (!grid_fits(workgroups(cut.job[0]) + workgroups(cut.job[1]), cut.job[0].wide ? 512 : 256) || !grid_fits(row_wgs + gather_wgs, 256)) return TC_ERR_SHAPE;
+  // many_kernel gathers itself where its workgroups have all rows and all keys of a group
+  const bool gathers = a.weight && cut.parts == 1 && cut.job[0].many && cut.job[0].tiles == 1;
   Job few[2] = {};
   int nf = 0;
   for (int k = 0; k < cut.jobs; k++) {
@@ -1147,7 +1219,8 @@ static int attention_launch(const CachePlan& pl, AttnArgs a, hipStream_t st) {
       continue;
     }
     if constexpr (sizeof(T) == 2) {
-      const auto kernel = cut.job[k].rows <= MROWS / 2 ? many_kernel<T, DH, 2> : many_kernel<T, DH, 1>;
+      const auto kernel = cut.job[k].rows <= MROWS / 2 ? (gathers ? many_kernel<T, DH, 2, true> : many_kernel<T, DH, 2, false>)
+                                                       : (gathers ? many_kernel<T, DH, 1, true> : many_kernel<T, DH, 1, false>);
       if (!allow_lds(kernel, ManyShape<DH>::LDS)) return TC_ERR_HIP;
       kernel<<<(unsigned)workgroups(cut.job[k]), 256, ManyShape<DH>::LDS, st>>>(a, cut.job[k]);
     }
@@ -1165,7 +1238,7 @@ static int attention_launch(const CachePlan& pl, AttnArgs a, hipStream_t st) {
     return check_launch();  // (a single part: few_kernel has gathered)
   }
   if (a.parts > 1) join_kernel<T, DH><<<row_wgs, 256, 0, st>>>(a);
-  if (a.weight) {
+  if (a.weight && !gathers) {
     bool done = false;
     if constexpr (sizeof(T) == 2) {
       done = pl.R > GATHER_ROWS;
