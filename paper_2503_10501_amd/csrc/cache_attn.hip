@@ -507,7 +507,8 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(AttnArgs a, Job first, 
 // 64 x 40 heads of 128, 576 rows, 640 keys, bf16: 475 to 515 us, 540 TFLOP/s of what is seen (tiles of 64 keys by 128 rows compute a fifth more
 // at the diagonal; 2048 rows of 16000 keys: 960).  Two wavefronts on a SIMD have 2048 cycles of products and 2300 of vector work a pair of tiles, the LDS of a
 // compute unit 2560, which overlap by half.  64 rows a wavefront (half of the LDS reads, one wavefront on a SIMD) took 850 us, the keys two tiles ahead
-// in L2 617, a priority for the products changed nothing.  With 64 rows a workgroup, heads of 64 (1024 groups of 61 rows, 640 + 90 keys): 28 us.
+// in L2 617, a priority for the products changed nothing.  With 64 rows a workgroup, heads of 64 (1024 groups of 61 rows, 640 + 90 keys): 28 us, 30 with
+// the weights, which a kernel of their own took 8 for.
 constexpr int MK = 64, MROWS = 128;
 template <int DH>
 struct ManyShape {
@@ -952,12 +953,13 @@ __global__ __launch_bounds__(256) void join_gather_kernel(AttnArgs a, int row_wg
   if (k < n) add_weights(a, bh, k, n, tokens_of(a, b), lse);
 }
 
-// What slots gather where rows are many: 32 keys per wavefront, kept in registers; the rows of queries pass by, GR of 16 at a time, whose loads are
-// issued together.  The keys and the first rows come before the length is known.  (1024 heads of 64, 61 rows, up to 90 slots, half: 8.4 us; a chain of
-// loads and the products of one or two rounds.)
+// What slots gather where rows are many and many_kernel has not added it.  float32: 32 keys per wavefront, kept in registers; the rows of queries pass by,
+// GR of 16 at a time, whose loads are issued together.  The keys and the first rows come before the length is known.  Products of four float32 elements and their
+// loads bound it (128 heads of 64, 40 rows, up to 3000 slots: 39 us).
 constexpr int GR = 2, GK = 128;  // (GK: keys of a workgroup)
-template <typename T, int DH>
+template <int DH>
 __global__ __launch_bounds__(256) void gather_kernel(AttnArgs a, Div by_chunks) {
+  typedef float T;
   typedef Mma<T> M;
   typedef typename M::frag frag;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
@@ -1019,10 +1021,10 @@ __global__ __launch_bounds__(256) void gather_kernel(AttnArgs a, Div by_chunks) 
   }
 }
 
-// ... of more rows than GATHER_ROWS in 16-bit storage: 128 keys a workgroup, 32 of them in a wavefront's registers as the operand of 32 x 32 tiles; 64
-// rows at a time pass through LDS for all four (two stages, as in many_kernel).  Rows that see none of the keys are not fetched.  (The scores are formed
-// a second time, since kept they would be 4 bytes for each: 64 x 40 heads, 576 rows, 640 keys: 440 us beside the 515 of the attention.)
-constexpr int GATHER_ROWS = 64;
+// 16-bit storage: 128 keys a workgroup, 32 of them in a wavefront's registers as the operand of 32 x 32 tiles; 64 rows at a time pass through LDS for all
+// four (two stages, as in many_kernel).  Rows that see none of the keys are not fetched.  The scores are formed a second time, since kept they
+// would be 4 bytes for each.  (64 x 40 heads of 128, 576 rows, 640 keys: 345 us beside the 500 of the attention.  128 heads of 64, 40 rows, up to 3000
+// keys in parts: 15; with the rows in registers, as for float32, 19.5.)
 template <typename T, int DH>
 __global__ __launch_bounds__(256, 2) void gather_many_kernel(AttnArgs a, Div by_chunks) {
   typedef Mma<T> M;
@@ -1239,12 +1241,9 @@ static int attention_launch(const CachePlan& pl, AttnArgs a, hipStream_t st) {
   }
   if (a.parts > 1) join_kernel<T, DH><<<row_wgs, 256, 0, st>>>(a);
   if (a.weight && !gathers) {
-    bool done = false;
-    if constexpr (sizeof(T) == 2) {
-      done = pl.R > GATHER_ROWS;
-      if (done) gather_many_kernel<T, DH><<<(unsigned)gather_wgs, 256, 0, st>>>(a, Div((uint32_t)chunks));
-    }
-    if (!done) gather_kernel<T, DH><<<(unsigned)gather_wgs, 256, 0, st>>>(a, Div((uint32_t)chunks));
+    const Div by_chunks((uint32_t)chunks);
+    if constexpr (sizeof(T) == 2) gather_many_kernel<T, DH><<<(unsigned)gather_wgs, 256, 0, st>>>(a, by_chunks);
+    else gather_kernel<DH><<<(unsigned)gather_wgs, 256, 0, st>>>(a, by_chunks);
   }
   return check_launch();
 }

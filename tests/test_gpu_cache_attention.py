@@ -191,6 +191,15 @@ def test_peaked_and_scaled_scores(dtype):
     check(make(dtype, 64, 2, 2, 2, 33, 200, [200, 111], scale=1e-3, images=1, P=64))
 
 
+@pytest.mark.parametrize("dtype,d,G,T,P", [("bf16", 64, 1, 20, 0), ("f16", 64, 2, 32, 70), ("bf16", 128, 1, 33, 0), ("f16", 128, 4, 25, 40)])
+def test_heads_enough_that_keys_are_one_part(dtype, d, G, T, P):
+    # (what the slots gather is then added by the kernel that attends, several tiles of keys one after another)
+    g = np.random.default_rng(T)
+    B, Hk, cap = 16, 32, 330
+    lens = [330, 0, 1, 64, 65, 128, 129, 192, 193] + [int(x) for x in g.integers(0, cap + 1, B - 9)]
+    check(make(dtype, d, B, G * Hk, Hk, T, cap, lens, [T, 0, T] + [int(x) for x in g.integers(0, T + 1, B - 3)], images=4 if P else 0, P=P, seed=T))
+
+
 @pytest.mark.parametrize("T", [1, 16, 40, 80])
 def test_many_halves_far_below_the_largest(T):
     """One key has all but a thousandth of the attention, 40000 others 2^-25.4 of its each: rounded to halves as they are they would be nothing.
