@@ -146,6 +146,7 @@ struct Job {
   int groups, rows, tiles, splits, part0;  // part0: the first of the `splits` parts that this share writes
   bool packed, prefix, cache, many;        // many: by many_kernel
   bool wide;                               // eight wavefronts
+  int share;                               // tiles of a workgroup at most
   Div by_splits, by_tiles;
 };
 
@@ -260,7 +261,7 @@ __device__ inline void add_weights(const AttnArgs& a, int group, int k, int n, i
     if (k + e < n) w[e] += acc[e];
 }
 
-// ---- few rows: one workgroup has 16 rows, its four or eight wavefronts share the keys, 32 at a time, without waiting for one another ----
+// ---- few rows: one workgroup has 16 rows, its one to eight wavefronts share the keys, 32 at a time, without waiting for one another ----
 //
 // The keys' and values' bytes bound it: each is read once, as whole lines, to registers while the tile before it is in work, and passes through LDS that
 // is the wavefront's own, so that no barrier stands between loads.  bf16, heads of 128: 64 sequences of 32 heads sharing 8 prefixes of 640 keys, up to
@@ -1134,12 +1135,13 @@ constexpr int FEW_ROWS = 16;
 static Job make_job(const CachePlan& pl, int groups, int rows, int keys, bool packed, bool prefix, bool cache, bool alone) {
   const bool many = rows > FEW_ROWS && pl.esize == 2;
   const int per = !many ? FEW_ROWS : rows <= MROWS / 2 ? MROWS / 2 : MROWS, tile = many ? MK : FK, least = many ? 2 : 4;
-  Job j = {groups, rows, (rows + per - 1) / per, 1, 0, packed, prefix, cache, many, false, Div(1), Div(1)};
+  Job j = {groups, rows, (rows + per - 1) / per, 1, 0, packed, prefix, cache, many, false, 0, Div(1), Div(1)};
   j.by_tiles = Div((uint32_t)j.tiles);
   const long long items = (long long)groups * j.tiles, tiles = (keys + tile - 1) / tile + (prefix && cache ? 1 : 0);
   // Few rows on a part of the chip, up to 768 keys: eight wavefronts take all keys, and nothing has to be joined.  (One sequence, 32 heads,
   // us in one sweep and in parts: 640 keys 10.5 and 11.9, 1000 14.3 and 12.5, 2000 21 and 15.)
   j.wide = !many && alone && items <= 256 && tiles > 4 && tiles <= 24 && !(pl.esize == 4 && pl.dh == 128);
+  j.share = (int)tiles;
   if (j.wide) return j;
   // Parts of the keys: two workgroups for each compute unit, if there is a tile for each wavefront (many: two for the workgroup).  Few rows
   // of long caches take four of them, which evens out sequences of different lengths, where a wavefront still has four tiles.  (us, two and
@@ -1152,6 +1154,7 @@ static Job make_job(const CachePlan& pl, int groups, int rows, int keys, bool pa
     if (t > s) s = t;
   }
   j.splits = s < 1 ? 1 : (int)s;
+  j.share = (int)((tiles + j.splits - 1) / j.splits);
   j.by_splits = Div((uint32_t)j.splits);
   return j;
 }
@@ -1229,11 +1232,23 @@ static int attention_launch(const CachePlan& pl, AttnArgs a, hipStream_t st) {
   }
   if (nf > 0) {
     typedef FewShape<T, DH> F;
-    const int waves = few[0].wide ? F::MOST : 4;
-    const auto kernel = waves == 8 ? (a.score ? few_kernel<T, DH, true, F::MOST> : few_kernel<T, DH, false, F::MOST>)
-                                   : (a.score ? few_kernel<T, DH, true, 4> : few_kernel<T, DH, false, 4>);
-    if (!allow_lds(kernel, waves * F::WAVE)) return TC_ERR_HIP;
-    kernel<<<(unsigned)(workgroups(few[0]) + workgroups(few[1])), 64 * waves, waves * F::WAVE, st>>>(a, few[0], few[1]);
+    // Where there are more workgroups than fit on the chip at once, and each has few tiles, one or two wavefronts have them: more are resident, no
+    // wavefront is idle and there is less to join.  (1960 heads of 128, bf16, us by 1, 2 and 4 wavefronts: 10 keys 12, 17 and 28; 160 keys
+    // 32, 35 and 40; 300 keys 58, 60 and 64; 700 keys 157, 154 and 151.  2048 heads of 200 keys and 256 prefixes of 640: 48, 46 and 54.)
+    const long long wgs = workgroups(few[0]) + workgroups(few[1]);
+    const int share = few[0].share > few[1].share ? few[0].share : few[1].share;
+    const bool crowded = wgs > 256 * (160 * 1024 / (4 * F::WAVE + 1024));
+    const int waves = few[0].wide ? F::MOST : crowded && share <= 6 ? 1 : crowded && share <= 10 ? 2 : 4;
+    auto launch = [&](auto kernel) -> int {
+      if (!allow_lds(kernel, waves * F::WAVE)) return TC_ERR_HIP;
+      kernel<<<(unsigned)wgs, 64 * waves, waves * F::WAVE, st>>>(a, few[0], few[1]);
+      return TC_OK;
+    };
+    const int rc = waves == 1 ? launch(a.score ? few_kernel<T, DH, true, 1> : few_kernel<T, DH, false, 1>)
+                 : waves == 2 ? launch(a.score ? few_kernel<T, DH, true, 2> : few_kernel<T, DH, false, 2>)
+                 : waves == 4 ? launch(a.score ? few_kernel<T, DH, true, 4> : few_kernel<T, DH, false, 4>)
+                              : launch(a.score ? few_kernel<T, DH, true, F::MOST> : few_kernel<T, DH, false, F::MOST>);
+    if (rc != TC_OK) return rc;
   }
   if (a.score) {
     if (a.parts > 1) join_gather_kernel<T, DH><<<(unsigned)(row_wgs + gather_wgs), 256, 0, st>>>(a, row_wgs, Div((uint32_t)chunks));

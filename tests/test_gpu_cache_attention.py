@@ -200,6 +200,17 @@ def test_heads_enough_that_keys_are_one_part(dtype, d, G, T, P):
     check(make(dtype, d, B, G * Hk, Hk, T, cap, lens, [T, 0, T] + [int(x) for x in g.integers(0, T + 1, B - 3)], images=4 if P else 0, P=P, seed=T))
 
 
+@pytest.mark.parametrize("dtype,d,B,G,T,cap,images,P", [
+    ("bf16", 128, 24, 1, 1, 40, 0, 0), ("f16", 128, 20, 4, 3, 170, 4, 20), ("bf16", 128, 24, 2, 1, 320, 0, 0), ("f16", 64, 40, 1, 2, 130, 0, 0),
+    ("bf16", 64, 40, 1, 1, 300, 8, 10), ("f32", 64, 24, 1, 1, 100, 2, 33), ("f32", 128, 12, 2, 5, 290, 0, 0), ("bf16", 128, 64, 1, 1, 60, 8, 40),
+    ("f16", 128, 64, 1, 1, 250, 8, 40)])
+def test_more_heads_than_fit_at_once(dtype, d, B, G, T, cap, images, P):
+    # (one or two wavefronts have a head's keys)
+    g = np.random.default_rng(cap)
+    lens = [cap, 0, 1, 33] + [int(x) for x in g.integers(0, cap + 1, B - 4)]
+    check(make(dtype, d, B, 32 * G, 32, T, cap, lens, [int(x) for x in g.integers(0, T + 1, B)] if T > 1 else None, images=images, P=P, seed=cap))
+
+
 @pytest.mark.parametrize("T", [1, 16, 40, 80])
 def test_many_halves_far_below_the_largest(T):
     """One key has all but a thousandth of the attention, 40000 others 2^-25.4 of its each: rounded to halves as they are they would be nothing.
