@@ -1134,7 +1134,7 @@ __global__ __launch_bounds__(256, 2) void gather_many_kernel(AttnArgs a, Div by_
 constexpr int FEW_ROWS = 16;
 static Job make_job(const CachePlan& pl, int groups, int rows, int keys, bool packed, bool prefix, bool cache, bool alone) {
   const bool many = rows > FEW_ROWS && pl.esize == 2;
-  const int per = !many ? FEW_ROWS : rows <= MROWS / 2 ? MROWS / 2 : MROWS, tile = many ? MK : FK, least = many ? 2 : 4;
+  const int per = !many ? FEW_ROWS : rows <= MROWS / 2 ? MROWS / 2 : MROWS, tile = many ? MK : FK, least = 4;
   Job j = {groups, rows, (rows + per - 1) / per, 1, 0, packed, prefix, cache, many, false, 0, Div(1), Div(1)};
   j.by_tiles = Div((uint32_t)j.tiles);
   const long long items = (long long)groups * j.tiles, tiles = (keys + tile - 1) / tile + (prefix && cache ? 1 : 0);
@@ -1143,10 +1143,12 @@ static Job make_job(const CachePlan& pl, int groups, int rows, int keys, bool pa
   j.wide = !many && alone && items <= 256 && tiles > 4 && tiles <= 24 && !(pl.esize == 4 && pl.dh == 128);
   j.share = (int)tiles;
   if (j.wide) return j;
-  // Parts of the keys: two workgroups for each compute unit, if there is a tile for each wavefront (many: two for the workgroup).  Few rows
+  // Parts of the keys: two workgroups for each compute unit, if there are four tiles for each.  Many rows: no more than two, since a second round of
+  // workgroups costs what the parts spare, and their joining more (us, with up to three and two: 96 heads of 592 rows and 540 keys 89 and 56; 64 of 552
+  // rows and 532 keys 68 and 49; 120 of 108 rows and 111 keys, where parts had two tiles, 29 and 13).  Few rows
   // of long caches take four of them, which evens out sequences of different lengths, where a wavefront still has four tiles.  (us, two and
   // four: 4 sequences of up to 32768 keys 99 and 94; one 24 and 29; 64 sequences sharing 8 prefixes of 640 keys 52 and 57.)
-  long long s = (512 + items - 1) / items;
+  long long s = many ? 512 / items : (512 + items - 1) / items;
   if (s > (tiles + least - 1) / least) s = (tiles + least - 1) / least;
   if (!many) {
     long long t = (1024 + items - 1) / items;

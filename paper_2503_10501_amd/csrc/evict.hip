@@ -256,8 +256,9 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const int32_t* __restri
   }
 }
 
-// The most slots of the variants that keep keys in registers.
-constexpr int EV_SMALL = 256 * 4, EV_MIDDLE = 512 * 8, EV_LARGE = 1024 * 32;
+// The most slots of the variants that keep keys in registers.  (1136 heads of up to 1790 slots: 36 us by 512 threads a head, 26 by 256; 256 heads of 2944
+// 41 by 512 threads, 42 by 1024, 45 by 256.)
+constexpr int EV_SMALL = 256 * 4, EV_HALF = 256 * 8, EV_MIDDLE = 512 * 8, EV_LARGE = 1024 * 32;
 
 size_t evict_bytes(const CachePlan& pl) {  // where rows come from; beyond the registers the list of survivors
   return (size_t)pl.B * pl.Hk * pl.budget * 4 * (pl.cap > EV_LARGE ? 2 : 1);
@@ -292,7 +293,7 @@ extern "C" int tc_cache_evict(const tc_cache* c, const int32_t* len, const void*
                  pos_out, weight_out, vecs};
   const bool fused = same == 4 && pl.max_len - pl.budget <= EV_FUSED;
   const int rows = 256 / vecs, most = pl.max_len < pl.budget ? pl.max_len : pl.budget, chunks = (most + rows - 1) / rows;
-  const int threads = pl.max_len <= EV_SMALL ? 256 : pl.max_len <= EV_MIDDLE ? 512 : 1024;
+  const int threads = pl.max_len <= EV_HALF ? 256 : pl.max_len <= EV_MIDDLE ? 512 : 1024;
   if (!grid_fits(heads, threads) || (!fused && !grid_fits((long long)heads * chunks, 256))) return TC_ERR_SHAPE;
 #define TC_EVICT(NT_, KPT_)                                        \
   do {                                                             \
@@ -303,6 +304,8 @@ extern "C" int tc_cache_evict(const tc_cache* c, const int32_t* len, const void*
   } while (0)
   if (pl.max_len <= EV_SMALL)
     TC_EVICT(256, 4);
+  else if (pl.max_len <= EV_HALF)
+    TC_EVICT(256, 8);
   else if (pl.max_len <= EV_MIDDLE)
     TC_EVICT(512, 8);
   else if (pl.max_len <= EV_LARGE)

@@ -191,3 +191,10 @@ def test_refusals():
     assert e.value.status == -2
     with pytest.raises(tc.TokenCarveError):
         tc.tc_cache_evict(tc.make_cache(1, 1, 1, 64, tc.TC_BF16, 1, 8), **t)
+
+
+@pytest.mark.parametrize("cap,budget", [(2048, 1024), (2049, 1024), (2048, 2047), (2049, 2000)])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_sizes_at_2048_slots(cap, budget, in_place):
+    # eight slots a thread, by 256 and by 512 threads
+    _run("bf16", 64, 2, 1, cap, [cap, max(0, cap - 1)], budget, sink=budget // 5, recent=budget // 3, in_place=in_place, shuffled=True)
