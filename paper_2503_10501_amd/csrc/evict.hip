@@ -257,8 +257,9 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const int32_t* __restri
 }
 
 // The most slots of the variants that keep keys in registers.  (1136 heads of up to 1790 slots: 36 us by 512 threads a head, 26 by 256; 256 heads of 2944
-// 41 by 512 threads, 42 by 1024, 45 by 256.)
-constexpr int EV_SMALL = 256 * 4, EV_HALF = 256 * 8, EV_MIDDLE = 512 * 8, EV_LARGE = 1024 * 32;
+// 41 by 512 threads, 42 by 1024, 45 by 256.  8 heads of up to 8000 and 12000 slots, with 8 and 16 keys a thread 20 and 28; with 32, whose masks pass the
+// scalar registers, 58 and 56.)
+constexpr int EV_SMALL = 256 * 4, EV_HALF = 256 * 8, EV_MIDDLE = 512 * 8, EV_DOUBLE = 1024 * 8, EV_QUADRUPLE = 1024 * 16, EV_LARGE = 1024 * 32;
 
 size_t evict_bytes(const CachePlan& pl) {  // where rows come from; beyond the registers the list of survivors
   return (size_t)pl.B * pl.Hk * pl.budget * 4 * (pl.cap > EV_LARGE ? 2 : 1);
@@ -308,6 +309,10 @@ extern "C" int tc_cache_evict(const tc_cache* c, const int32_t* len, const void*
     TC_EVICT(256, 8);
   else if (pl.max_len <= EV_MIDDLE)
     TC_EVICT(512, 8);
+  else if (pl.max_len <= EV_DOUBLE)
+    TC_EVICT(1024, 8);
+  else if (pl.max_len <= EV_QUADRUPLE)
+    TC_EVICT(1024, 16);
   else if (pl.max_len <= EV_LARGE)
     TC_EVICT(1024, 32);
   else

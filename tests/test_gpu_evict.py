@@ -198,3 +198,10 @@ def test_refusals():
 def test_sizes_at_2048_slots(cap, budget, in_place):
     # eight slots a thread, by 256 and by 512 threads
     _run("bf16", 64, 2, 1, cap, [cap, max(0, cap - 1)], budget, sink=budget // 5, recent=budget // 3, in_place=in_place, shuffled=True)
+
+
+@pytest.mark.parametrize("cap,budget", [(4097, 4096), (8192, 1000), (8193, 1000), (16384, 8000), (16385, 8000), (16384, 16383)])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_sizes_of_long_caches(cap, budget, in_place):
+    # eight, sixteen and more slots a thread
+    _run("f16", 64, 2, 1, cap, [cap, max(0, cap - 1)], budget, sink=budget // 5, recent=budget // 3, in_place=in_place, shuffled=True)
