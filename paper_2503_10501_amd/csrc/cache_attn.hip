@@ -1216,8 +1216,11 @@ static int attention_launch(const CachePlan& pl, AttnArgs a, hipStream_t st) {
   const int per = a.score ? GW : GK;
   const long long chunks = ((long long)pl.max_len + per - 1) / per, gather_wgs = a.weight ? chunks * pl.B * pl.Hk : 0;
   if (!grid_fits(workgroups(cut.job[0]) + workgroups(cut.job[1]), cut.job[0].wide ? 512 : 256) || !grid_fits(row_wgs + gather_wgs, 256)) return TC_ERR_SHAPE;
-  // many_kernel gathers itself where its workgroups have all rows and all keys of a group
-  const bool gathers = a.weight && cut.parts == 1 && cut.job[0].many && cut.job[0].tiles == 1;
+  // many_kernel gathers itself where its workgroups have all rows and all keys of a group, but for more than 64 rows of heads of 128: two wavefronts
+  // on a SIMD, each with a chain of loads and products, take longer than a kernel of its own (us, 1024 heads: 100 rows of 64, 640 + 150 keys, 54 and 61;
+  // 128 rows of 128, 1000 keys, 242 and 215; 40 rows of 128, 300 keys, 2048 heads, 106 and 110).
+  constexpr bool WIDE_ROWS = DH == 64;
+  const bool gathers = a.weight && cut.parts == 1 && cut.job[0].many && cut.job[0].tiles == 1 && (WIDE_ROWS || cut.job[0].rows <= MROWS / 2);
   Job few[2] = {};
   int nf = 0;
   for (int k = 0; k < cut.jobs; k++) {
@@ -1227,7 +1230,7 @@ static int attention_launch(const CachePlan& pl, AttnArgs a, hipStream_t st) {
     }
     if constexpr (sizeof(T) == 2) {
       const auto kernel = cut.job[k].rows <= MROWS / 2 ? (gathers ? many_kernel<T, DH, 2, true> : many_kernel<T, DH, 2, false>)
-                                                       : (gathers ? many_kernel<T, DH, 1, true> : many_kernel<T, DH, 1, false>);
+                                                       : (WIDE_ROWS && gathers ? many_kernel<T, DH, 1, WIDE_ROWS> : many_kernel<T, DH, 1, false>);
       if (!allow_lds(kernel, ManyShape<DH>::LDS)) return TC_ERR_HIP;
       kernel<<<(unsigned)workgroups(cut.job[k]), 256, ManyShape<DH>::LDS, st>>>(a, cut.job[k]);
     }
