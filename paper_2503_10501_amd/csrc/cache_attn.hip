@@ -265,7 +265,7 @@ __device__ inline void add_weights(const AttnArgs& a, int group, int k, int n, i
 //
 // The keys' and values' bytes bound it: each is read once, as whole lines, to registers while the tile before it is in work, and passes through LDS that
 // is the wavefront's own, so that no barrier stands between loads.  bf16, heads of 128: 64 sequences of 32 heads sharing 8 prefixes of 640 keys, up to
-// 200 slots: 46 us; 4 sequences of 8 heads for 32, up to 32768 slots: 84 us, 5.0 TB/s (a copy reaches 5.1).  One sequence of 32 heads and 640
+// 200 slots: 39 us; 4 sequences of 8 heads for 32, up to 32768 slots: 84 us, 4.9 TB/s (a copy reaches 5.1).  One sequence of 32 heads and 640
 // slots: 9.9 us, of which the chain launch, length, two or three tiles, joining of eight wavefronts is nearly all.
 
 constexpr int FK = 32;  // keys of a wavefront's tile
@@ -1147,7 +1147,7 @@ static Job make_job(const CachePlan& pl, int groups, int rows, int keys, bool pa
   // workgroups costs what the parts spare, and their joining more (us, with up to three and two: 96 heads of 592 rows and 540 keys 89 and 56; 64 of 552
   // rows and 532 keys 68 and 49; 120 of 108 rows and 111 keys, where parts had two tiles, 29 and 13).  Few rows
   // of long caches take four of them, which evens out sequences of different lengths, where a wavefront still has four tiles.  (us, two and
-  // four: 4 sequences of up to 32768 keys 99 and 94; one 24 and 29; 64 sequences sharing 8 prefixes of 640 keys 52 and 57.)
+  // four: 4 sequences of up to 32768 keys 99 and 94; one 24 and 29.)
   long long s = many ? 512 / items : (512 + items - 1) / items;
   if (s > (tiles + least - 1) / least) s = (tiles + least - 1) / least;
   if (!many) {
@@ -1217,7 +1217,7 @@ static int attention_launch(const CachePlan& pl, AttnArgs a, hipStream_t st) {
   const long long chunks = ((long long)pl.max_len + per - 1) / per, gather_wgs = a.weight ? chunks * pl.B * pl.Hk : 0;
   if (!grid_fits(workgroups(cut.job[0]) + workgroups(cut.job[1]), cut.job[0].wide ? 512 : 256) || !grid_fits(row_wgs + gather_wgs, 256)) return TC_ERR_SHAPE;
   // many_kernel gathers itself where its workgroups have all rows and all keys of a group, but for more than 64 rows of heads of 128: two wavefronts
-  // on a SIMD, each with a chain of loads and products, take longer than a kernel of its own (us, 1024 heads: 100 rows of 64, 640 + 150 keys, 54 and 61;
+  // on a SIMD, each with a chain of loads and products, take longer than a kernel of its own (us, here and there, 1024 heads: 100 rows of 64, 640 + 150 keys, 54 and 61;
   // 128 rows of 128, 1000 keys, 242 and 215; 40 rows of 128, 300 keys, 2048 heads, 106 and 110).
   constexpr bool WIDE_ROWS = DH == 64;
   const bool gathers = a.weight && cut.parts == 1 && cut.job[0].many && cut.job[0].tiles == 1 && (WIDE_ROWS || cut.job[0].rows <= MROWS / 2);
