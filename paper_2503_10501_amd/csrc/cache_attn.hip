@@ -720,7 +720,7 @@ __global__ __launch_bounds__(256, KW == 2 && DH == 64 ? 4 : 2) void many_kernel(
     if (!idle && k0 < (pre ? a.P : wave_most)) {
       const bool masked = k0 + MK / KW > (pre ? a.P : wave_least);
       w.step(Ks + ku * S::KLD, Ks + MK * S::KLD + ku * S::VLD, k0, lim, masked, a.scale2, offset, lane);
-      if (masked && __builtin_amdgcn_readfirstlane(flag[t % 3]))
+      if (__builtin_amdgcn_readfirstlane(flag[t % 3]))  // (where the tile was changed, which goes by what all rows of the workgroup see)
         w.add_odd(static_cast<const T*>(pre ? a.Vp : a.Vc) + ((pre ? phead : head) + k0) * DH, min(MK / KW, (pre ? a.P : most) - k0), lim - k0, lane);
     }
     if (tid == 0) flag[(t + 2) % 3] = 0;  // (last looked at before the last barrier, set again behind the next one)

@@ -1,0 +1,71 @@
+"""Infinities and NaN among the values that attention over the cache reads: they reach every row that sees them, in the element they are in, and nothing else."""
+import pytest
+import torch
+
+from tests.test_gpu_cache_attention import call, make
+
+pytestmark = pytest.mark.gpu
+
+NAN, INF = float("nan"), float("inf")
+
+
+def planted(s, spots):
+    """Plants (tensor, sequence or image, key, element, value) in all heads and returns, per output, the sum of what its row sees of them (0: nothing)."""
+    c = s["c"]
+    B, T, H, d = c.batch, c.n_query, c.n_heads, c.head_dim
+    seen = torch.zeros(B, T, H, d)
+    t = torch.arange(T)
+    for name, i, key, e, value in spots:
+        s[name][i, :, key, e] = value
+        for b in range(B):
+            n, m = int(s["lens"][b]), T if s["q_len"] is None else int(s["q_len"][b])
+            if name == "Vp":
+                rows = (t < m) & (b // (B // c.n_prefixes) == i)
+            else:
+                rows = (t < m) & (key <= n - m + t) & (b == i)
+            seen[b, rows, :, e] += value
+    return seen.cuda()
+
+
+def compare(build, spots, before=None):
+    """Outputs and weights with the values and without: what sees none of them is the same bit by bit."""
+    s, t = build(), build()
+    if before is not None:
+        before(s)
+        before(t)
+    seen = planted(t, spots)
+    call(s)
+    call(t)
+    torch.cuda.synchronize()
+    clean, got = (x["O"].view(seen.shape) for x in (s, t))
+    assert clean.isfinite().all()
+    touched = seen != 0     # (NaN too)
+    assert touched.any() and torch.equal(got[~touched], clean[~touched])
+    hit, want = got[touched].float(), seen[touched]
+    lost = torch.where(want.isnan(), ~hit.isnan(), hit != want)
+    assert not lost.any(), "%d of %d" % (int(lost.sum()), lost.numel())
+    if s["w"] is not None:
+        assert torch.equal(s["w"], t["w"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("value", [NAN, INF, -INF])
+@pytest.mark.parametrize("T,n,P,spot", [
+    (20, 30, 40, ("Vp", 3)), (60, 70, 40, ("Vp", 3)), (20, 30, 100, ("Vp", 70)),         # a prefix that ends inside a tile, two wavefronts share its keys
+    (60, 90, 0, ("V", 5)), (40, 90, 100, ("V", 10)), (40, 90, 100, ("Vp", 95)),          # slots that the first rows of a tile do not see all of
+    (128, 256, 0, ("V", 140)), (128, 228, 0, ("V", 70)), (128, 228, 0, ("V", 101)),      # 128 rows: wavefronts of rows that see the tile whole
+    (300, 340, 33, ("V", 200)), (300, 340, 33, ("V", 339)), (576, 640, 0, ("V", 77))])
+def test_many_rows_that_see_a_tile_whole_beside_rows_that_do_not(dtype, d, value, T, n, P, spot):
+    compare(lambda: make(dtype, d, 2, 1, 1, T, n + 5, [n, n - 3], [T, T - 2], images=1 if P else 0, P=P, seed=T), [(spot[0], 0, spot[1], 11, value)])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d,T,G", [(64, 40, 1), (64, 100, 1), (128, 40, 1), (64, 25, 4), (128, 300, 2)])
+@pytest.mark.parametrize("B,Hk", [(2, 2), (16, 32)])
+def test_many_rows_and_several_values_at_once(dtype, d, T, G, B, Hk):
+    # infinities of both signs in one element are no number, in others they stay apart; keys in parts (few heads) and in one part
+    n = T + 140
+    spots = [("Vp", 0, 3, 0, INF), ("V", 0, 70, 1, -INF), ("V", 0, n - T + 2, 1, -INF), ("V", 0, n - 1, 2, NAN), ("V", 1, 100, 3, INF),
+             ("V", 1, n - T + 5, 3, -INF), ("Vp", 0, 50, d - 1, -INF)]
+    compare(lambda: make(dtype, d, B, G * Hk, Hk, T, n, [n] * B, images=2, P=52, seed=d), spots)
