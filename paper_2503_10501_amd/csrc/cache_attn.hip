@@ -218,6 +218,41 @@ __device__ inline bool any_not_finite(const u4& w) {
   return bad;
 }
 
+// Values that are not finite.  In tiles of which some row does not see all, they are kept out of the product (0 times them is NaN), in others the product
+// takes them as they come, and a probability that has become 0, or whose head and remainder differ in sign, makes NaN of an infinity.  So behind the
+// last tile a wavefront that has met one sets what it has found right: an element of a row's output is the sum of such values among those that the row
+// sees, if there are any.
+
+// A partial output's element times a factor of the softmax, 0 .. 1: what is not finite stays so where the factor has become 0.
+__device__ inline float scaled(float x, float f) {
+  const float y = x * f;
+  return y == y ? y : x;
+}
+
+// Whether a value of these rows is not finite, by a wavefront.
+template <typename T, int DH>
+__device__ inline bool any_odd(const T* V, int rows, int lane) {
+  const u4* v = reinterpret_cast<const u4*>(V);
+  bool odd = false;
+#pragma unroll 4
+  for (int at = lane; at < rows * (DH * (int)sizeof(T) / 16); at += 64) odd |= any_not_finite<T>(v[at]);
+  return __ballot(odd) != 0;
+}
+
+// Adds the values that are not finite among elements `first` + STEP j .. + 3 of rows 0 .. min(rows, lim) - 1 to sum[j].
+template <typename T, int DH, int STEP>
+__device__ inline void add_odd(const T* V, int rows, int lim, int first, f4 (&sum)[DH / STEP]) {
+#pragma unroll 1
+  for (int k = 0; k < rows; k++)
+#pragma unroll
+    for (int j = 0; j < DH / STEP; j++)
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const T v = V[(size_t)k * DH + first + STEP * j + e];
+        if (k < lim && not_finite(v)) sum[j][e] += Vec16<T>::one(v);
+      }
+}
+
 // Rows of keys and values from `first` on to registers, N threads side by side: they are one run of 16-byte vectors.  Behind the `there` rows
 // that exist the last vector of these is read; of values zero stands in its place (zero_behind) before they are used.
 template <int N, int VEC, int NV>
@@ -342,6 +377,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(AttnArgs a, Job first, 
 #pragma unroll
   for (int d = 0; d < DT; d++) o[d] = f4{0.f, 0.f, 0.f, 0.f};
   float mx = -INFINITY, sum = 0.f;
+  bool odd = false;  // a value that is not finite was kept out of a product
 
   int t = t0 + wave;
   if (!ahead && t < t1) fetch(t);
@@ -349,13 +385,13 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(AttnArgs a, Job first, 
     const bool pre = t < np;
     const int k0 = (pre ? t : t - np) * FK, last = pre ? a.P : most;
     const bool masked = k0 + FK > (pre ? a.P : least);  // some row does not see some key
-    bool odd = false;                                    // a value that is not finite where rows differ in what they see
     if (masked) {
       zero_behind<64, VEC>(last - k0, lane, vr);
+      bool found = false;
 #pragma unroll
-      for (int j = 0; j < NV; j++) odd |= any_not_finite<T>(vr[j]);
-      odd = __ballot(odd) != 0;
-      if (odd) {
+      for (int j = 0; j < NV; j++) found |= any_not_finite<T>(vr[j]);
+      if (__ballot(found)) {
+        odd = true;
 #pragma unroll
         for (int j = 0; j < NV; j++) vr[j] = finite_only<T>(vr[j]);
       }
@@ -434,20 +470,32 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(AttnArgs a, Job first, 
       o[d] = M::mul(v, ph, o[d]);
       if constexpr (sizeof(T) == 2) o[d] = M::mul(v, pr, o[d]);
     }
-    if (odd) {  // these reach the rows that see them, and no other
-      const T* V = static_cast<const T*>(pre ? a.Vp : a.Vc) + ((pre ? phead : head) + k0) * DH;
-      const int keys = min(FK, last - k0), lim = (pre ? last : end) - k0;
-#pragma unroll 1
-      for (int k = 0; k < keys; k++)
-#pragma unroll
-        for (int d = 0; d < DT; d++)
-#pragma unroll
-          for (int e = 0; e < 4; e++) {
-            const T v = V[(size_t)k * DH + 16 * d + 4 * g + e];
-            if (k < lim && not_finite(v)) o[d][e] += Vec16<T>::one(v);
-          }
-    }
     wave_lds_order();
+  }
+  if (!odd) {
+    f4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int d = 0; d < DT; d++)
+#pragma unroll
+      for (int e = 0; e < 4; e++) z[e] = fmaf(o[d][e], 0.f, z[e]);
+    odd = __ballot(live && z[0] + z[1] + z[2] + z[3] != 0.f) != 0;
+  }
+  if (__builtin_expect(odd, 0)) {
+    f4 add[DT];
+#pragma unroll
+    for (int d = 0; d < DT; d++) add[d] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int u = t0 + wave; u < t1; u += WAVES) {
+      const bool pre = u < np;
+      const int k0 = (pre ? u : u - np) * FK, keys = min(FK, (pre ? a.P : most) - k0);
+      const T* V = static_cast<const T*>(pre ? a.Vp : a.Vc) + ((pre ? phead : head) + k0) * DH;
+      if (any_odd<T, DH>(V, keys, lane)) add_odd<T, DH, 16>(V, keys, (pre ? a.P : end) - k0, 4 * g, add);
+    }
+#pragma unroll
+    for (int d = 0; d < DT; d++)
+#pragma unroll
+      for (int e = 0; e < 4; e++)
+        if (add[d][e] != 0.f) o[d][e] = add[d][e];
   }
   sum = col_sum(sum);
 
@@ -466,7 +514,14 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(AttnArgs a, Job first, 
   const float f = exp2_fast(mx - ref);
   float* part = reinterpret_cast<float*>(cache_smem + wave * S::WAVE);
 #pragma unroll
-  for (int d = 0; d < DT; d++) *reinterpret_cast<f4*>(part + i * (DH + 4) + 16 * d + 4 * g) = o[d] * f;
+  for (int d = 0; d < DT; d++) {
+    f4 v = o[d] * f;
+    if (odd) {
+#pragma unroll
+      for (int e = 0; e < 4; e++) v[e] = scaled(o[d][e], f);
+    }
+    *reinterpret_cast<f4*>(part + i * (DH + 4) + 16 * d + 4 * g) = v;
+  }
   if (threadIdx.x < 16 && mine) {  // (wavefront 0, lane i: row i)
     const float lse = live ? ref + a.offset + log2f(total) : INFINITY;
     if (a.parts > 1) a.ml[(size_t)(job.part0 + split) * a.rows + row] = f2{top == -INFINITY ? top : top + a.offset, total};
@@ -601,19 +656,6 @@ struct ManyWave {
       }
     }
   }
-
-  // Values that are not finite, which the tile has zero for, reach the rows that see them, and no other.
-  __device__ __forceinline__ void add_odd(const T* V, int keys, int lim, int lane) {
-#pragma unroll 1
-    for (int k = 0; k < keys; k++)
-#pragma unroll
-      for (int d = 0; d < DH / 32; d++)
-#pragma unroll
-        for (int e = 0; e < 16; e++) {
-          const T v = V[(size_t)k * DH + 32 * d + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)];
-          if (k < lim && not_finite(v)) o[d][e] += Vec16<T>::one(v);
-        }
-  }
 };
 
 // GATHER: the workgroup has all rows of its group and all of their keys, and adds what the slots gather itself, from scores formed again, with the keys
@@ -625,7 +667,7 @@ __global__ __launch_bounds__(256, KW == 2 && DH == 64 ? 4 : 2) void many_kernel(
   constexpr int ROWS = MROWS / KW, RW = 4 / KW;  // rows of the workgroup, wavefronts that share them
   const float offset = a.offset + LAZY;          // (a probability may pass that of the running maximum so far)
   extern __shared__ __attribute__((aligned(16))) unsigned char cache_smem[];
-  __shared__ int flag[3];
+  __shared__ int odd_values;  // some were kept out of a product, or have come out of one
   __shared__ size_t places[4][32];  // of rows in the output
   // where it gathers: behind the outputs, in the place of the tiles
   constexpr int KEYS = 32 * Wave::NU, GBYTES = ROWS * 8 + 2 * 4 * KEYS * 4;
@@ -666,7 +708,7 @@ __global__ __launch_bounds__(256, KW == 2 && DH == 64 ? 4 : 2) void many_kernel(
     seen_by(a, max(tile0, 0), tile0 + ROWS - 1, n, m, least, most);
     seen_by(a, max(r0, 0), max(r0 + 31, 0), n, m, wave_least, wave_most);
   }
-  if (tid < 3) flag[tid] = 0;
+  if (tid == 0) odd_values = 0;
   __syncthreads();
   const int np = job.prefix && m > 0 ? (a.P + MK - 1) / MK : 0, all = m > 0 ? np + (most + MK - 1) / MK : 0;
   int t0, t1;
@@ -688,7 +730,7 @@ __global__ __launch_bounds__(256, KW == 2 && DH == 64 ? 4 : 2) void many_kernel(
 #pragma unroll
       for (int j = 0; j < S::NV; j++) odd |= any_not_finite<T>(vr[j]);
       if (odd) {
-        flag[t % 3] = 1;
+        odd_values = 1;
 #pragma unroll
         for (int j = 0; j < S::NV; j++) vr[j] = finite_only<T>(vr[j]);
       }
@@ -720,11 +762,8 @@ __global__ __launch_bounds__(256, KW == 2 && DH == 64 ? 4 : 2) void many_kernel(
     if (!idle && k0 < (pre ? a.P : wave_most)) {
       const bool masked = k0 + MK / KW > (pre ? a.P : wave_least);
       w.step(Ks + ku * S::KLD, Ks + MK * S::KLD + ku * S::VLD, k0, lim, masked, a.scale2, offset, lane);
-      if (__builtin_amdgcn_readfirstlane(flag[t % 3]))  // (where the tile was changed, which goes by what all rows of the workgroup see)
-        w.add_odd(static_cast<const T*>(pre ? a.Vp : a.Vc) + ((pre ? phead : head) + k0) * DH, min(MK / KW, (pre ? a.P : most) - k0), lim - k0, lane);
     }
-    if (tid == 0) flag[(t + 2) % 3] = 0;  // (last looked at before the last barrier, set again behind the next one)
-    if (t + 1 < t1) store(t + 1);         // the other stage was last read before the last barrier
+    if (t + 1 < t1) store(t + 1);  // the other stage was last read before the last barrier
     __syncthreads();
     if (t + 2 < t1) fetch(t + 2);
   }
@@ -751,6 +790,32 @@ __global__ __launch_bounds__(256, KW == 2 && DH == 64 ? 4 : 2) void many_kernel(
       for (int e = 0; e < 16; e++) w.o[d][e] = w.o[d][e] * f0 + at[64 * (2 + 16 * d + e)] * f1;
     w.mx = mx;
     wave_lds_order();
+  }
+  bool odd = __builtin_amdgcn_readfirstlane(odd_values) != 0;
+  if (!odd) {
+    f4 z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int d = 0; d < DH / 32; d++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) z[e % 4] = fmaf(w.o[d][e], 0.f, z[e % 4]);
+    odd = __ballot(live && z[0] + z[1] + z[2] + z[3] != 0.f) != 0;
+  }
+  if (__builtin_expect(odd && !idle && wave % RW == wave, 0)) {
+    f4 add[DH / 8];
+#pragma unroll
+    for (int j = 0; j < DH / 8; j++) add[j] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int t = t0; t < t1; t++) {
+      const bool pre = t < np;
+      const int k0 = (pre ? t : t - np) * MK, keys = min(MK, (pre ? a.P : wave_most) - k0);
+      const T* V = static_cast<const T*>(pre ? a.Vp : a.Vc) + ((pre ? phead : head) + k0) * DH;
+      if (any_odd<T, DH>(V, keys, lane)) add_odd<T, DH, 8>(V, keys, (pre ? a.P : end) - k0, 4 * half, add);
+    }
+#pragma unroll
+    for (int d = 0; d < DH / 32; d++)
+#pragma unroll
+      for (int e = 0; e < 16; e++)
+        if (add[4 * d + e / 4][e % 4] != 0.f) w.o[d][e] = add[4 * d + e / 4][e % 4];
   }
   if (a.parts > 1) {
     if (!mine) return;
@@ -884,7 +949,14 @@ __device__ inline void join_row(const AttnArgs& a, int row, float* lds) {
   for (int s = p; s < a.parts; s += GR) {
     const f2 x = a.ml[(size_t)s * a.rows + row];
     if (x[0] == -INFINITY && x[1] == 0.f) continue;  // saw nothing: its part is not written
-    v += exp2_fast(x[0] - ref) * *reinterpret_cast<const f4*>(a.part + ((size_t)s * a.rows + row) * DH + 4 * c);
+    const f4 y = *reinterpret_cast<const f4*>(a.part + ((size_t)s * a.rows + row) * DH + 4 * c);
+    const float f = exp2_fast(x[0] - ref);
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+      const float x = v[e];
+      v[e] += f * y[e];
+      if (v[e] != v[e]) v[e] = x + scaled(y[e], f);
+    }
   }
 #pragma unroll
   for (int e = 0; e < 4; e++)

@@ -69,3 +69,41 @@ def test_many_rows_and_several_values_at_once(dtype, d, T, G, B, Hk):
     spots = [("Vp", 0, 3, 0, INF), ("V", 0, 70, 1, -INF), ("V", 0, n - T + 2, 1, -INF), ("V", 0, n - 1, 2, NAN), ("V", 1, 100, 3, INF),
              ("V", 1, n - T + 5, 3, -INF), ("Vp", 0, 50, d - 1, -INF)]
     compare(lambda: make(dtype, d, B, G * Hk, Hk, T, n, [n] * B, images=2, P=52, seed=d), spots)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("value", [NAN, INF, -INF])
+@pytest.mark.parametrize("T,n,P,spots", [
+    (1, 300, 0, [("V", 0), ("V", 299)]), (1, 300, 0, [("V", 70)]), (1, 8, 200, [("Vp", 5)]), (1, 8, 200, [("Vp", 199)]), (3, 130, 40, [("Vp", 33), ("V", 129)]),
+    (16, 90, 0, [("V", 40)]), (16, 90, 70, [("V", 80), ("Vp", 64)]), (1, 7000, 0, [("V", 4000)]), (5, 7000, 100, [("Vp", 10)])])
+def test_few_rows_wherever_the_value_lies(dtype, d, value, T, n, P, spots):
+    # a tile that all rows see whole, one that they do not, keys of one workgroup and in parts
+    spots = [(name, 0, key, 3 + i, value) for i, (name, key) in enumerate(spots)]
+    compare(lambda: make(dtype, d, 2, 2, 1, T, n, [n, n - 1], images=1 if P else 0, P=P, seed=n), spots)
+
+
+@pytest.mark.parametrize("dtype,d,each,T", [("bf16", 128, 20, 1), ("bf16", 128, 7, 2), ("f16", 64, 40, 2), ("f32", 64, 20, 1)])
+def test_a_prefix_that_is_read_once(dtype, d, each, T):
+    P, Hk = 1200, 16
+    assert 2 * (each - 1) * Hk * P * d * 2 * torch.finfo({"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}[dtype]).bits // 8 >= 32e6
+    g = torch.Generator().manual_seed(each)
+    lens = [int(x) for x in torch.randint(T, 60, (2 * each,), generator=g)]
+    spots = [("Vp", 0, 5, 0, INF), ("Vp", 1, 700, 1, NAN), ("Vp", 1, P - 1, 2, -INF), ("V", 3, 0, 3, INF), ("Vp", 0, 9, 3, -INF)]
+    compare(lambda: make(dtype, d, 2 * each, Hk, Hk, T, 60, lens, images=2, P=P, seed=each), spots)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("T,n,P", [(1, 300, 0), (4, 90, 200), (1, 7000, 0), (40, 300, 0), (40, 90, 100), (200, 700, 0)])
+@pytest.mark.parametrize("rising", [True, False])
+def test_however_small_its_probability_is(dtype, T, n, P, rising):
+    """Scores along the keys rise or fall by 640, so that probabilities of float32 are 0 at one end, and what was summed there is scaled to 0 on the way."""
+    def ramp(s):
+        s["Q"].zero_()
+        s["Q"][..., 0] = 64.0
+        for name, keys in (("Kp", P), ("K", n)):
+            if keys:
+                x = torch.linspace(-40.0, 40.0, P + n)[:P] if name == "Kp" else torch.linspace(-40.0, 40.0, P + n)[P:]
+                s[name][..., :keys, 0] = (x if rising else -x).to(s[name].dtype).cuda()
+    spots = [("V", 0, 2, 0, INF), ("V", 0, n - T, 1, -INF), ("V", 1, n // 2 - T, 2, NAN)] + ([("Vp", 0, 7, 3, INF), ("Vp", 0, P - 1, 4, -INF)] if P else [])
+    compare(lambda: make(dtype, 64, 2, 2, 2, T, n, [n, n], images=1 if P else 0, P=P, seed=n), spots, ramp)
