@@ -94,6 +94,15 @@ __device__ inline float col_sum(float x) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// What is subtracted from scores whose largest is `top`: top + offset (AttnArgs).  Scores beyond 2^24 round this sum; where an offset below 0 would grow by it,
+// probabilities could pass the range of half, and it is left out.
+template <typename T>
+__device__ inline float reference(float top, float offset) {
+  const float r = top + offset;
+  if constexpr (Mma<T>::WIDE) return r;
+  else return top - r > -offset ? top : r;
+}
+
 // The value of the lane that a data-parallel permutation pairs this one with, within 16 lanes.
 template <int CTRL>
 __device__ inline float lane_of(float x) {
@@ -274,6 +283,9 @@ __device__ __forceinline__ void zero_behind(int there, int id, u4 (&vr)[NV]) {
     if (id + N * j >= there * VEC) vr[j] = u4{0, 0, 0, 0};
 }
 
+// A sum of probabilities of the R rows: no more than R of them, which the rounding of a logarithm beyond 2^24 could make of it (NaN stays).
+__device__ inline float share(const AttnArgs& a, float sum) { return sum > (float)a.R ? (float)a.R : sum; }
+
 // Slots k .. k + 3 of a sequence and head gather the probabilities of its few rows, from the scores that were kept.  A row's scores are there up to
 // the tile that the last row sees; what lies behind what the row sees is read and left out (loads under conditions would wait for one another:
 // 2 sequences of 10 rows 4.8 us of 11.5).
@@ -293,7 +305,7 @@ __device__ inline void add_weights(const AttnArgs& a, int group, int k, int n, i
   }
 #pragma unroll
   for (int e = 0; e < 4; e++)
-    if (k + e < n) w[e] += acc[e];
+    if (k + e < n) w[e] += share(a, acc[e]);
 }
 
 // ---- few rows: one workgroup has 16 rows, its one to eight wavefronts share the keys, 32 at a time, without waiting for one another ----
@@ -426,9 +438,9 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(AttnArgs a, Job first, 
       for (int u = 0; u < 2; u++) *reinterpret_cast<f4*>(to + 16 * u) = s[u];
     }
     top = fmaxf(mx, col_max(top));
-    const float ref = top == -INFINITY ? 0.f : top + a.offset;
+    const float ref = top == -INFINITY ? 0.f : reference<T>(top, a.offset);
     if (__ballot(top > mx)) {
-      const float f = exp2_fast(mx + a.offset - ref);
+      const float f = exp2_fast(reference<T>(mx, a.offset) - ref);
       sum *= f;
 #pragma unroll
       for (int d = 0; d < DT; d++) o[d] *= f;
@@ -500,6 +512,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(AttnArgs a, Job first, 
   sum = col_sum(sum);
 
   // the wavefronts' parts
+  mx = reference<T>(mx, a.offset);  // (-inf of nothing)
   if (g == 0) {
     wave_m[wave][i] = mx;
     wave_l[wave][i] = sum;
@@ -523,8 +536,8 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(AttnArgs a, Job first, 
     *reinterpret_cast<f4*>(part + i * (DH + 4) + 16 * d + 4 * g) = v;
   }
   if (threadIdx.x < 16 && mine) {  // (wavefront 0, lane i: row i)
-    const float lse = live ? ref + a.offset + log2f(total) : INFINITY;
-    if (a.parts > 1) a.ml[(size_t)(job.part0 + split) * a.rows + row] = f2{top == -INFINITY ? top : top + a.offset, total};
+    const float lse = live ? ref + log2f(total) : INFINITY;
+    if (a.parts > 1) a.ml[(size_t)(job.part0 + split) * a.rows + row] = f2{top, total};
     else if (a.lse) a.lse[row] = lse;
     row_lse[i] = lse;
     row_sum[i] = live && a.P + end > 0 ? total : INFINITY;
@@ -576,6 +589,11 @@ struct ManyShape {
 // The running maximum is raised when a row's passes it by more than 2^8: up to there the probabilities are larger than 1, which neither
 // the sums in float32 nor the heads mind, and the partial output need not be scaled.
 constexpr float LAZY = 8.f;
+// The largest score is rounded, the product that the probabilities are formed of is not.  From here on they differ by what an exponent may not be off
+// by: a workgroup that has met such a score goes over its keys again with scores that are rounded before.
+constexpr float LARGE = 0x1p22f;
+
+template <bool B> struct Flag { static constexpr bool value = B; };
 
 template <typename T, int DH, int KW>
 struct ManyWave {
@@ -588,9 +606,10 @@ struct ManyWave {
   float mx, sum;
 
   // One tile.  `masked`: some row of the wavefront does not see some key; keys below `lim` are seen by this lane's row.  (One body for both: with
-  // two the partial output would move between registers.)
+  // two the partial output would move between registers.)  `large` is set where a score has reached LARGE, ROUNDED: scores are rounded.
+  template <bool ROUNDED>
   __device__ __forceinline__ void step(const unsigned char* Ks, const unsigned char* Vs, int k0, int lim, bool masked, float scale2, float offset,
-                                       int lane) {
+                                       int lane, int* large) {
     const int half = lane >> 5, i = lane & 31;
     f16v s[NU];
 #pragma unroll
@@ -606,6 +625,13 @@ struct ManyWave {
         k.u = *reinterpret_cast<const u4*>(kr + u * 32 * S::KLD + 32 * c);
         s[u] = M::mul32(k, q[c], s[u]);
       }
+    if constexpr (ROUNDED) {
+#pragma unroll
+      for (int u = 0; u < NU; u++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) s[u][e] *= scale2;
+      scale2 = 1.f;
+    }
     if (masked) {
 #pragma unroll
       for (int u = 0; u < NU; u++)
@@ -621,13 +647,14 @@ struct ManyWave {
     const u2 w = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
     top = fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1])) * scale2;
     if (__ballot(top > mx + LAZY)) {
-      const float now = fmaxf(mx, top), f = now == -INFINITY ? 1.f : exp2_fast(mx - now);
+      const float now = fmaxf(mx, top), f = now == -INFINITY ? 1.f : exp2_fast(reference<T>(mx, offset) - reference<T>(now, offset));
+      if (!ROUNDED && fabsf(now) >= LARGE && fabsf(now) < INFINITY) *large = 1;
       mx = now;
       sum *= f;
 #pragma unroll
       for (int d = 0; d < DH / 32; d++) o[d] *= f;
     }
-    const float ref = mx == -INFINITY ? 0.f : mx + offset;
+    const float ref = mx == -INFINITY ? 0.f : reference<T>(mx, offset);
 #pragma unroll
     for (int u = 0; u < NU; u++) {
       float p[16];
@@ -667,7 +694,7 @@ __global__ __launch_bounds__(256, KW == 2 && DH == 64 ? 4 : 2) void many_kernel(
   constexpr int ROWS = MROWS / KW, RW = 4 / KW;  // rows of the workgroup, wavefronts that share them
   const float offset = a.offset + LAZY;          // (a probability may pass that of the running maximum so far)
   extern __shared__ __attribute__((aligned(16))) unsigned char cache_smem[];
-  __shared__ int odd_values;  // some were kept out of a product, or have come out of one
+  __shared__ int large_scores, odd_values;  // of any row;  some were kept out of a product, or have come out of one
   __shared__ size_t places[4][32];  // of rows in the output
   // where it gathers: behind the outputs, in the place of the tiles
   constexpr int KEYS = 32 * Wave::NU, GBYTES = ROWS * 8 + 2 * 4 * KEYS * 4;
@@ -708,7 +735,7 @@ __global__ __launch_bounds__(256, KW == 2 && DH == 64 ? 4 : 2) void many_kernel(
     seen_by(a, max(tile0, 0), tile0 + ROWS - 1, n, m, least, most);
     seen_by(a, max(r0, 0), max(r0 + 31, 0), n, m, wave_least, wave_most);
   }
-  if (tid == 0) odd_values = 0;
+  if (tid == 0) large_scores = odd_values = 0;
   __syncthreads();
   const int np = job.prefix && m > 0 ? (a.P + MK - 1) / MK : 0, all = m > 0 ? np + (most + MK - 1) / MK : 0;
   int t0, t1;
@@ -743,30 +770,36 @@ __global__ __launch_bounds__(256, KW == 2 && DH == 64 ? 4 : 2) void many_kernel(
     }
   };
 
+  auto sweep = [&](auto rounded) __attribute__((always_inline)) {
+    constexpr bool ROUNDED = decltype(rounded)::value;
 #pragma unroll
-  for (int d = 0; d < DH / 32; d++)
+    for (int d = 0; d < DH / 32; d++)
 #pragma unroll
-    for (int e = 0; e < 16; e++) w.o[d][e] = 0.f;
-  w.mx = -INFINITY;
-  w.sum = 0.f;
-  if (t0 < t1) {
-    if (!ahead) fetch(t0);
-    store(t0);
-    if (t0 + 1 < t1) fetch(t0 + 1);
-    __syncthreads();
-  }
-  for (int t = t0; t < t1; t++) {
-    const bool pre = t < np;
-    const int k0 = (pre ? t : t - np) * MK + ku, lim = pre ? a.P : end;
-    const unsigned char* Ks = cache_smem + (t & 1) * S::STAGE;
-    if (!idle && k0 < (pre ? a.P : wave_most)) {
-      const bool masked = k0 + MK / KW > (pre ? a.P : wave_least);
-      w.step(Ks + ku * S::KLD, Ks + MK * S::KLD + ku * S::VLD, k0, lim, masked, a.scale2, offset, lane);
+      for (int e = 0; e < 16; e++) w.o[d][e] = 0.f;
+    w.mx = -INFINITY;
+    w.sum = 0.f;
+    if (t0 < t1) {
+      if (ROUNDED || !ahead) fetch(t0);
+      store(t0);
+      if (t0 + 1 < t1) fetch(t0 + 1);
+      __syncthreads();
     }
-    if (t + 1 < t1) store(t + 1);  // the other stage was last read before the last barrier
-    __syncthreads();
-    if (t + 2 < t1) fetch(t + 2);
-  }
+    for (int t = t0; t < t1; t++) {
+      const bool pre = t < np;
+      const int k0 = (pre ? t : t - np) * MK + ku, lim = pre ? a.P : end;
+      const unsigned char* Ks = cache_smem + (t & 1) * S::STAGE;
+      if (!idle && k0 < (pre ? a.P : wave_most)) {
+        const bool masked = k0 + MK / KW > (pre ? a.P : wave_least);
+        w.template step<ROUNDED>(Ks + ku * S::KLD, Ks + MK * S::KLD + ku * S::VLD, k0, lim, masked, a.scale2, offset, lane, &large_scores);
+      }
+      if (t + 1 < t1) store(t + 1);  // the other stage was last read before the last barrier
+      __syncthreads();
+      if (t + 2 < t1) fetch(t + 2);
+    }
+  };
+  sweep(Flag<false>());
+  if (__builtin_expect(t0 < t1 && __builtin_amdgcn_readfirstlane(large_scores), 0)) sweep(Flag<true>());
+  w.mx = reference<T>(w.mx, offset);  // (-inf of nothing)
   const u2 x = __builtin_amdgcn_permlane32_swap(__float_as_uint(w.sum), __float_as_uint(w.sum), false, false);
   float total = __uint_as_float(x[0]) + __uint_as_float(x[1]);
   if constexpr (KW == 2) {  // the second wavefront of the rows hands its share to the first (behind the last barrier nobody reads the tiles)
@@ -820,7 +853,7 @@ __global__ __launch_bounds__(256, KW == 2 && DH == 64 ? 4 : 2) void many_kernel(
   if (a.parts > 1) {
     if (!mine) return;
     const size_t at = (size_t)(job.part0 + split) * a.rows + row;
-    if (half == 0) a.ml[at] = f2{w.mx == -INFINITY ? w.mx : w.mx + offset, total};
+    if (half == 0) a.ml[at] = f2{w.mx, total};
     if (t0 >= t1) return;
 #pragma unroll
     for (int d = 0; d < DH / 32; d++)
@@ -830,7 +863,7 @@ __global__ __launch_bounds__(256, KW == 2 && DH == 64 ? 4 : 2) void many_kernel(
     return;
   }
   if (!GATHER && idle) return;
-  const float lse = live ? (w.mx == -INFINITY ? 0.f : w.mx) + offset + log2f(total) : INFINITY;
+  const float lse = live ? (w.mx == -INFINITY ? 0.f : w.mx) + log2f(total) : INFINITY;
   // keys of the slots as operands, 32 of a wavefront's in each run: lane i has part of slot k0 + i
   typename Mma<T>::frag ks[GATHER ? Wave::NU : 1][DH / 16];
   auto load_slots = [&](int k0) {
@@ -907,7 +940,7 @@ __global__ __launch_bounds__(256, KW == 2 && DH == 64 ? 4 : 2) void many_kernel(
         float all = 0.f;
 #pragma unroll
         for (int x = 0; x < RW; x++) all += now[(tid / KEYS * RW + x) * KEYS + tid % KEYS];
-        a.weight[head + k0 + tid] += all;
+        a.weight[head + k0 + tid] += share(a, all);
       }
     }
   }
@@ -1090,7 +1123,7 @@ __global__ __launch_bounds__(256) void gather_kernel(AttnArgs a, Div by_chunks) 
       acc[u][e] += lane_of<0x140>(acc[u][e]);  // 15 - L of each 16
     }
     const int at = k0 + 16 * u + 4 * g + i;
-    if (i < 4 && at < n) a.weight[(size_t)bh * a.cap + at] += i == 0 ? acc[u][0] : i == 1 ? acc[u][1] : i == 2 ? acc[u][2] : acc[u][3];
+    if (i < 4 && at < n) a.weight[(size_t)bh * a.cap + at] += share(a, i == 0 ? acc[u][0] : i == 1 ? acc[u][1] : i == 2 ? acc[u][2] : acc[u][3]);
   }
 }
 
@@ -1198,7 +1231,7 @@ __global__ __launch_bounds__(256, 2) void gather_many_kernel(AttnArgs a, Div by_
     if (i == 0) sums[wave][8 * (e >> 2) + 4 * half + (e & 3)] = __uint_as_float(w[0]) + __uint_as_float(w[1]);
   }
   wave_lds_order();
-  if (lane < 32 && k0 + lane < n) a.weight[(size_t)bh * a.cap + k0 + lane] += sums[wave][lane];
+  if (lane < 32 && k0 + lane < n) a.weight[(size_t)bh * a.cap + k0 + lane] += share(a, sums[wave][lane]);
 }
 
 // How a call is cut.  The prefix of an image's sequences is read once for all of them where the rows of one sequence do not fill a
