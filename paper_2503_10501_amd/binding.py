@@ -351,7 +351,10 @@ def tc_rope_tables(r, pos_ids, cos, sin, stream=None):
 
 
 def tc_rope_apply(r, x, cos, sin, y=None, transposed=False, stream=None):
-    """x, y: [batch, heads, rows, head_dim] views; without y the rows of x are turned in place."""
+    """x, y: [batch, heads, rows, head_dim] views; without y the rows of x are turned in place.  No call of this module is recorded for
+    gradients; this one, whose gradient is the transposed turn, refuses tensors that require them unless they are switched off (torch.no_grad)."""
+    if torch.is_grad_enabled() and (x.requires_grad or (y is not None and y.requires_grad)):
+        raise ValueError("x, y: the turn is not recorded for gradients: call it under torch.no_grad(), its gradient is transposed=True")
     dev, sd, shape = _device("x", x), x.dtype, x.shape
     if x.dim() != 4 or shape[3] != r.head_dim:
         raise ValueError("x: expected [batch, heads, rows, %d], got %s" % (r.head_dim, tuple(shape)))
