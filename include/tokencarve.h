@@ -332,7 +332,8 @@ typedef struct {
 } tc_rope;
 
 /* Strides of a [batch, head, row, d_h] tensor, in elements; the elements of a row are contiguous.  Every stride is >= 0 and a
-   multiple of 16 bytes (so [B, T, H, d_h] and parts of a packed projection will do); inputs may repeat rows (stride 0). */
+   multiple of 16 bytes (so [B, T, H, d_h] and parts of a packed projection will do); inputs may repeat rows (stride 0), rows that are
+   written may not overlap (a stride below d_h, where there is more than one entry along it, is refused). */
 typedef struct {
   int64_t batch, head, row;
 } tc_strides;

@@ -41,12 +41,12 @@ inline bool known_dtype(int dtype) { return dtype == TC_F32 || dtype == TC_BF16 
 int check_rope(const tc_rope* r);  // tc_status
 inline int rope_dim(const tc_rope* r) { return r->rot_dim > 0 ? r->rot_dim : r->head_dim; }
 
-// Strides along which there is more than one entry (`output`: entries that are written, which must differ).
-inline bool bad_strides(const tc_strides* s, int esize, int batch, int heads, int rows, bool output) {
+// Strides along which there is more than one entry (`output`: rows of `width` elements that are written, which must not overlap).
+inline bool bad_strides(const tc_strides* s, int esize, int batch, int heads, int rows, int width, bool output) {
   const int64_t v[3] = {s->batch, s->head, s->row};
   const int n[3] = {batch, heads, rows};
   for (int i = 0; i < 3; i++)
-    if (n[i] > 1 && (v[i] < 0 || v[i] > (int64_t(1) << 44) || v[i] * esize % 16 != 0 || (output && v[i] == 0))) return true;
+    if (n[i] > 1 && (v[i] < 0 || v[i] > (int64_t(1) << 44) || v[i] * esize % 16 != 0 || (output && v[i] < width))) return true;
   return false;
 }
 

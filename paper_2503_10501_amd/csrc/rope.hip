@@ -289,7 +289,7 @@ extern "C" int tc_rope_apply(const tc_rope* r, int32_t dtype, int32_t batch, int
   if (batch == 0 || n_rows == 0) return TC_OK;
   if (!x || !xs || !cos || !sin || !y || !ys) return TC_ERR_NULL;
   const int es = elem_size(dtype);
-  if (bad_strides(xs, es, batch, n_heads, n_rows, false) || bad_strides(ys, es, batch, n_heads, n_rows, true)) return TC_ERR_SHAPE;
+  if (bad_strides(xs, es, batch, n_heads, n_rows, r->head_dim, false) || bad_strides(ys, es, batch, n_heads, n_rows, r->head_dim, true)) return TC_ERR_SHAPE;
   if (misaligned(x) || misaligned(cos) || misaligned(sin) || misaligned(y)) return TC_ERR_ALIGN;
   if (x == y && ((batch > 1 && xs->batch != ys->batch) || (n_heads > 1 && xs->head != ys->head) || (n_rows > 1 && xs->row != ys->row)))
     return TC_ERR_PARAM;
@@ -308,8 +308,8 @@ extern "C" int tc_cache_append(const tc_cache* cache, const tc_rope* r, const vo
   if (pl.B == 0) return TC_OK;
   if (!Q || !qs || !K || !ks || !V || !vs || !pos_ids || !len || !Q_out || !K_cache || !V_cache || !slot_pos || !weight) return TC_ERR_NULL;
   if ((cos == nullptr) != (r == nullptr) || (sin == nullptr) != (r == nullptr)) return TC_ERR_NULL;
-  if (bad_strides(qs, pl.esize, pl.B, pl.H, pl.T, false) || bad_strides(ks, pl.esize, pl.B, pl.Hk, pl.T, false) ||
-      bad_strides(vs, pl.esize, pl.B, pl.Hk, pl.T, false))
+  if (bad_strides(qs, pl.esize, pl.B, pl.H, pl.T, pl.dh, false) || bad_strides(ks, pl.esize, pl.B, pl.Hk, pl.T, pl.dh, false) ||
+      bad_strides(vs, pl.esize, pl.B, pl.Hk, pl.T, pl.dh, false))
     return TC_ERR_SHAPE;
   if (misaligned(Q) || misaligned(K) || misaligned(V) || misaligned(cos) || misaligned(sin) || misaligned(pos_ids) || misaligned(len) ||
       misaligned(q_len) || misaligned(Q_out) || misaligned(K_cache) || misaligned(V_cache) || misaligned(slot_pos) || misaligned(weight))
