@@ -382,7 +382,8 @@ typedef struct {
 } tc_cache;
 
 /* Bytes of scratch that any entry point may need for `c` (0 if c is invalid), whatever max_len is.  Where H/H_kv * T <= 16 there are 4 bytes
-   for each query row and slot among them (scores that tc_cache_attention keeps for the weights).  budget is looked at only by
+   for each query row and slot of the capacity among them (scores that tc_cache_attention keeps for the weights), also for a caller
+   who passes no weight.  budget is looked at only by
    tc_cache_evict: 0 will do elsewhere. */
 TC_API size_t tc_cache_workspace_bytes(const tc_cache* c);
 
@@ -417,7 +418,9 @@ TC_API int tc_cache_append(const tc_cache* c, const tc_rope* r, const void* Q, c
  * logarithm of a row's sum in float32, so relatively off by 2^-24 of a score's size in base 2: by percents from 2^20 on, and beyond 2^24 only
  * bounded, by 0 and the number of rows.  No two tensors overlap.  16-bit storage: probabilities enter
  * their products as a 16-bit head and remainder in tiles of up to 16 rows, rounded to 16 bits in larger ones (an error of the size of O's own
- * rounding).
+ * rounding).  What counts are the rows that read the same keys: H/H_kv * T of a sequence; at a prefix that is read once those of all its
+ * sequences, so that single tokens are rounded so too where more than 16 rows share such a prefix.  Rows behind q_len[b] are computed like tokens
+ * and cost as much.
  */
 TC_API int tc_cache_attention(const tc_cache* c, const void* Q, const void* K_prefix, const void* V_prefix, const void* K_cache,
                               const void* V_cache, const int32_t* len, const int32_t* q_len, void* O, float* weight, void* ws,
@@ -425,7 +428,7 @@ TC_API int tc_cache_attention(const tc_cache* c, const void* Q, const void* K_pr
 
 /*
  * Eviction: of every sequence and key/value head the `budget` best slots stay in use.  A slot whose position is below n_sink or above
- * newest - n_recent (newest: the largest position in use) comes before the others, these come by weight, largest first (NaN last), equal
+ * newest - n_recent (newest: the largest position in use) comes before the others, these come by weight, largest first (NaN as -infinity), equal
  * ones by slot, lowest first.  Slots 0 .. budget-1 that stay keep what they hold; the others that stay go, in ascending order, to the
  * slots that are freed there, in ascending order.  Where no more than `budget` slots are in use all of them stay.
  *   K_out, V_out [B, H_kv, out_capacity, d_h], pos_out, weight_out [B, H_kv, out_capacity]: written up to len_out[b], left as they are behind

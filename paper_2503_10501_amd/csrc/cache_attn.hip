@@ -313,7 +313,7 @@ __device__ inline void add_weights(const AttnArgs& a, int group, int k, int n, i
 // The keys' and values' bytes bound it: each is read once, as whole lines, to registers while the tile before it is in work, and passes through LDS that
 // is the wavefront's own, so that no barrier stands between loads.  bf16, heads of 128: 64 sequences of 32 heads sharing 8 prefixes of 640 keys, up to
 // 200 slots: 39 us; 4 sequences of 8 heads for 32, up to 32768 slots: 84 us, 4.9 TB/s (a copy reaches 5.1).  One sequence of 32 heads and 640
-// slots: 9.9 us, of which the chain launch, length, two or three tiles, joining of eight wavefronts is nearly all.
+// slots: 10.2 us, of which the chain launch, length, two or three tiles, joining of eight wavefronts is nearly all.
 
 constexpr int FK = 32;  // keys of a wavefront's tile
 template <typename T, int DH>
@@ -573,11 +573,12 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(AttnArgs a, Job first, 
 // operand of the second product wants.  A tile is in one of two stages of LDS while the next one is written into the other and the one
 // after that comes to registers: one barrier a tile.
 //
-// 64 x 40 heads of 128, 576 rows, 640 keys, bf16: 475 to 515 us, 540 TFLOP/s of what is seen (tiles of 64 keys by 128 rows compute a fifth more
-// at the diagonal; 2048 rows of 16000 keys: 960).  Two wavefronts on a SIMD have 2048 cycles of products and 2300 of vector work a pair of tiles, the LDS of a
+// 64 x 40 heads of 128, 576 rows, 640 keys, bf16: 469 us one after another, 570 TFLOP/s of what is seen (485 to 515 in single passes, at lower clocks; tiles of
+// 64 keys by 128 rows compute a fifth more at the diagonal; 40 heads, 2048 rows of 16000 keys: 766 us, 820).  Two wavefronts on a SIMD have 2048 cycles of products and 2300 of vector work a pair of tiles, the LDS of a
 // compute unit 2560, which overlap by half.  64 rows a wavefront (half of the LDS reads, one wavefront on a SIMD) took 850 us, the keys two tiles ahead
-// in L2 617, a priority for the products changed nothing.  With 64 rows a workgroup, heads of 64 (1024 groups of 61 rows, 640 + 90 keys): 28 us, 30 with
-// the weights, which a kernel of their own took 8 for.
+// in L2 617, a priority for the products changed nothing.  With 64 rows a workgroup, heads of 64 (1024 groups of 1 to 61 rows, 640 + 90 keys): 27 us, 32 with
+// the weights, which a kernel of their own took 8 for.  Rows behind q_len are computed like tokens: half of all rows here, and a quarter of the wavefronts has no
+// other.
 constexpr int MK = 64, MROWS = 128;
 template <int DH>
 struct ManyShape {
@@ -1129,7 +1130,7 @@ __global__ __launch_bounds__(256) void gather_kernel(AttnArgs a, Div by_chunks) 
 
 // 16-bit storage: 128 keys a workgroup, 32 of them in a wavefront's registers as the operand of 32 x 32 tiles; 64 rows at a time pass through LDS for all
 // four (two stages, as in many_kernel).  Rows that see none of the keys are not fetched.  The scores are formed a second time, since kept they
-// would be 4 bytes for each.  (64 x 40 heads of 128, 576 rows, 640 keys: 345 us beside the 500 of the attention.  128 heads of 64, 40 rows, up to 3000
+// would be 4 bytes for each.  (64 x 40 heads of 128, 576 rows, 640 keys: 296 us beside the 469 of the attention.  128 heads of 64, 40 rows, up to 3000
 // keys in parts: 15; with the rows in registers, as for float32, 19.5.)
 template <typename T, int DH>
 __global__ __launch_bounds__(256, 2) void gather_many_kernel(AttnArgs a, Div by_chunks) {

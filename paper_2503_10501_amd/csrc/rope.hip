@@ -42,8 +42,9 @@ __device__ inline void sin_cos(double x, double* sn, double* cs) {
   *cs = (k + 1) & 2 ? -b : b;
 }
 
-// One thread has one pair's angle per position, an exponential in float64, and goes over some positions: up to some thousand of them the launch
-// and one thread's chain of float64 operations bound it (64 pairs, 528 positions 3.2 us, 23552 positions 9.1 us for 12 MB).
+// One thread has one pair's angle per position, an exponential in float64, and goes over some positions, one after another: a load and some thirty
+// float64 operations that wait for each other.  Up to some thousand positions the launch and that chain bound it (16 pairs, 2103 positions 3.2 us; a single
+// position 2.0), above that the chains of up to eight positions a thread (64 pairs, 23552 positions 9.0 us for 12 MB, which alone would take 2.4).
 __global__ __launch_bounds__(256) void rope_tables_kernel(const int32_t* __restrict__ pos, long long n, float* __restrict__ c,
                                                           float* __restrict__ s, int half, double log_base, int scaling, double factor,
                                                           double original_len, double low, double high, double magnitude, int per) {
