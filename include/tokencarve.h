@@ -414,13 +414,13 @@ TC_API int tc_cache_append(const tc_cache* c, const tc_rope* r, const void* Q, c
  *   O         [B, T, H*d_h]             rows t >= q_len[b], and rows that see no key, are zero
  *   weight    [B, H_kv, capacity] float, read and written, sums in a fixed order; NULL: not wanted
  * What a row does not see has no influence on it, infinities and NaN included; a value that is not finite reaches its element of every row that
- * sees it at a finite score, however small the probability.  Finite scores of any size give finite outputs; what slots gather is formed with the
- * logarithm of a row's sum in float32, so relatively off by 2^-24 of a score's size in base 2: by percents from 2^20 on, and beyond 2^24 only
- * bounded, by 0 and the number of rows.  No two tensors overlap.  16-bit storage: probabilities enter
- * their products as a 16-bit head and remainder in tiles of up to 16 rows, rounded to 16 bits in larger ones (an error of the size of O's own
- * rounding).  What counts are the rows that read the same keys: H/H_kv * T of a sequence; at a prefix that is read once those of all its
- * sequences, so that single tokens are rounded so too where more than 16 rows share such a prefix.  Rows behind q_len[b] are computed like tokens
- * and cost as much.
+ * sees it at a finite score, however small the probability.  Finite scores of any size give finite outputs (beyond 2^27 in base 2 where a row's
+ * values add up within float32); what slots gather is formed with the logarithm of a row's sum in float32, so relatively off by 2^-24 of a
+ * score's size in base 2: by percents from 2^20 on, and beyond 2^24 only bounded, by 0 and the number of rows.
+ * No two tensors overlap.  Rows behind q_len[b] are computed like tokens and cost as much.
+ * 16-bit storage: probabilities enter their products as a 16-bit head and remainder in tiles of up to 16 rows, rounded to 16 bits in larger
+ * ones (an error of the size of O's own rounding).  What counts are the rows that read the same keys: H/H_kv * T of a sequence; at a prefix that is
+ * read once those of all its sequences, so that single tokens are rounded so too where more than 16 rows share such a prefix.
  */
 TC_API int tc_cache_attention(const tc_cache* c, const void* Q, const void* K_prefix, const void* V_prefix, const void* K_cache,
                               const void* V_cache, const int32_t* len, const int32_t* q_len, void* O, float* weight, void* ws,
