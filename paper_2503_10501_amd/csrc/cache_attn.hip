@@ -695,7 +695,7 @@ __global__ __launch_bounds__(256, KW == 2 && DH == 64 ? 4 : 2) void many_kernel(
   constexpr int ROWS = MROWS / KW, RW = 4 / KW;  // rows of the workgroup, wavefronts that share them
   const float offset = a.offset + LAZY;          // (a probability may pass that of the running maximum so far)
   extern __shared__ __attribute__((aligned(16))) unsigned char cache_smem[];
-  __shared__ int large_scores, odd_values;  // of any row;  some were kept out of a product, or have come out of one
+  __shared__ int large_scores, odd_values;  // a score has reached LARGE; values that are not finite were kept out of a product
   __shared__ size_t places[4][32];  // of rows in the output
   // where it gathers: behind the outputs, in the place of the tiles
   constexpr int KEYS = 32 * Wave::NU, GBYTES = ROWS * 8 + 2 * 4 * KEYS * 4;
